@@ -57,7 +57,7 @@ typedef enum {
     LKV_E_HIP = 7           /* the HIP runtime reported an error (lkv_last_hip_error) */
 } lkv_status;
 
-typedef enum { LKV_F32 = 0, LKV_BF16 = 1 } lkv_dtype;
+typedef enum { LKV_F32 = 0, LKV_BF16 = 1, LKV_E4M3 = 2 /* lkv_attn.cache_dtype only */ } lkv_dtype;
 typedef enum { LKV_GDN = 0, LKV_SSD = 1 } lkv_family;
 
 /* Geometry of one recurrent layer.
@@ -361,6 +361,119 @@ lkv_status lkv_gather_selected(const lkv_layer* layer, const lkv_tokens* ctx, co
 lkv_status lkv_state_rel_error(const float* S, const float* S_ref, int32_t n_slices,
                                int64_t slice_elems, int32_t group, double* sq, double* rel,
                                double* rel_group, void* stream);
+
+/* ---- Full-attention layers --------------------------------------------------
+ * A hybrid model's other layers attend over the whole context.  Position-
+ * independent caching concatenates the cached blocks' keys and values there
+ * and overwrites them at the recomputed positions U (Alg. 1), so these layers
+ * need: attention inside each block when the cache is built (or over a whole
+ * prompt), a paged cache in which a context is a list of pages, the write of
+ * U's keys and values into it, and attention of U's queries, at their own
+ * positions, over it; then decoding, which is the same with one token.
+ *
+ *   h_q, h_kv    query heads and key/value heads; query head h reads
+ *                key/value head h / (h_q / h_kv)
+ *   d            head dimension, in {64, 128, 256}
+ *   page         tokens per page, a power of two in [16, 1024] (prefill: unused
+ *                but checked)
+ *   io_dtype     dtype of q, k, v and o          LKV_F32 (d <= 128) | LKV_BF16
+ *   cache_dtype  dtype of the pages              io_dtype, or LKV_E4M3 with LKV_BF16
+ *   scale        softmax scale, finite and > 0
+ *
+ * A token at position p attends to its request's keys 0..p: with s_j = scale
+ * q.k_j, o = sum_j exp(s_j) v_j / sum_j exp(s_j).  Scores, statistics and sums
+ * are fp32; with bf16 tokens the probabilities are rounded to bf16 for the
+ * product with v.  A token that sees no key gives zeros.  Keys and values that
+ * a token does not see do not affect it, whatever they hold; if a value that it
+ * sees is infinite or NaN, that element of its output is not finite.
+ *
+ * Token arrays have rows [heads, d] `stride` elements apart (a multiple of 16
+ * bytes, at least heads * d), so q, k and v may be views of one projection's
+ * output; o is dense.  cu: device int32 [n_req+1], cu[0] = 0, non-decreasing;
+ * n_tok: host bound of cu[n_req].  Rows from cu[n_req] on are not touched, so
+ * a padded batch (a captured graph's) may pass its capacity. */
+typedef struct {
+    int32_t h_q;
+    int32_t h_kv;
+    int32_t d;
+    int32_t page;
+    int32_t io_dtype;
+    int32_t cache_dtype;
+    float scale;
+} lkv_attn;
+
+/* Paged cache of one layer.
+ *   k, v     [n_page, h_kv, page, d] cache_dtype, device
+ *   k_exp, v_exp  LKV_E4M3: [n_page, h_kv, page] uint8, device: a row of codes c
+ *            stands for c * 2^(exp - 127); otherwise NULL
+ *   table    device int32 [n_req, max_pages]: request r's token at position p is
+ *            in slot p % page of page table[r][p / page].  Entries past the
+ *            context are not read.  Requests may share pages.
+ *   len      device int32 [n_req]: tokens in each context, the new ones included
+ *            (clamped to [0, max_pages * page], and to 0 if n_page is 0)
+ * A page id outside [0, n_page) is never followed: a write to it is dropped, a
+ * read gives NaN rows, and attention gives NaN to every token that sees it (and
+ * may to the request's others). */
+typedef struct {
+    void* k;
+    void* v;
+    uint8_t* k_exp;
+    uint8_t* v_exp;
+    int32_t n_page;
+    int32_t max_pages;
+    const int32_t* table;
+    const int32_t* len;
+} lkv_pages;
+
+/* Causal attention over packed sequences (cached blocks, each on its own, or
+ * whole prompts): token i of a sequence attends to its tokens 0..i.
+ *   q [n_tok,h_q,d], k, v [n_tok,h_kv,d], o [n_tok,h_q,d] io_dtype
+ * Errors: LKV_E_NULL, LKV_E_SHAPE, LKV_E_DTYPE, LKV_E_ALIGN, LKV_E_UNSUPPORTED,
+ * LKV_E_HIP. */
+lkv_status lkv_attn_prefill(const lkv_attn* attn, const int32_t* cu, int32_t n_seq, int64_t n_tok,
+                            const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                            const void* v, int64_t v_stride, void* o, void* stream);
+
+/* Write tokens into the cache: request r's tokens cu[r]..cu[r+1] go to positions
+ * pos[cu[r]..cu[r+1]] of its context (device int32 [n_tok]), or, with pos NULL,
+ * to its last positions len[r] - (cu[r+1] - cu[r]).. .  A position outside
+ * [0, len[r]) is dropped.  Where a position occurs twice in a row in pos, its
+ * last token is written; other repetitions, and tokens of different requests
+ * that reach one slot, race.
+ * LKV_E4M3: a row x of d values is stored as codes e4m3(x * 2^-e), rounded to
+ * nearest even, with e the least integer in [-100, 120] such that max |x| <=
+ * 448 * 2^e; infinities and NaN do not count for e and become NaN.  (A power of
+ * two costs a floating-point code no precision, and what is read back, 4
+ * significant bits times 2^e, is exact in bf16.)
+ *   k, v  [n_tok,h_kv,d] io_dtype.  Errors as for lkv_attn_prefill. */
+lkv_status lkv_kv_write(const lkv_attn* attn, const lkv_pages* pages, const int32_t* cu, int32_t n_req,
+                        int64_t n_tok, const int32_t* pos, const void* k, int64_t k_stride,
+                        const void* v, int64_t v_stride, void* stream);
+
+/* Read rows of the cache back in io_dtype, by the same cu and pos (e.g. a
+ * cached block's rows for another context).  A position outside [0, len[r])
+ * gives NaN rows. */
+lkv_status lkv_kv_read(const lkv_attn* attn, const lkv_pages* pages, const int32_t* cu, int32_t n_req,
+                       int64_t n_tok, const int32_t* pos, void* k, int64_t k_stride, void* v,
+                       int64_t v_stride, void* stream);
+
+/* Attention of new tokens over the paged cache, which holds their own keys and
+ * values already (lkv_kv_write): request r's token i attends to positions
+ * 0..pos[cu[r] + i] (the recomputed tokens U, in any order), or, with pos NULL,
+ * to 0..len[r] - n_r + i: the last n_r tokens of the context -- a chunk of a
+ * prompt, drafted tokens, or one token, decoding.  A given position outside
+ * [0, len[r]) gives a NaN row; with pos NULL a position below 0 gives zeros.
+ *   q, o [n_tok,h_q,d] io_dtype
+ *   ws   device workspace of at least lkv_attn_paged_workspace bytes (for the
+ *        same n_req, n_tok and max_pages; may be NULL if that is 0), 256-byte
+ *        aligned, caller-owned; its contents on entry do not matter.  Calls that
+ *        share a workspace race unless ordered by a stream.
+ * Errors as for lkv_attn_prefill; LKV_E_SHAPE also for a workspace too small. */
+lkv_status lkv_attn_paged_workspace(const lkv_attn* attn, int32_t n_req, int64_t n_tok, int32_t max_pages,
+                                    size_t* bytes);
+lkv_status lkv_attn_paged(const lkv_attn* attn, const lkv_pages* pages, const int32_t* cu, int32_t n_req,
+                          int64_t n_tok, const int32_t* pos, const void* q, int64_t q_stride, void* o,
+                          void* ws, size_t ws_bytes, void* stream);
 
 #ifdef __cplusplus
 }

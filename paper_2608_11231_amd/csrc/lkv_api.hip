@@ -1,10 +1,12 @@
 // C ABI of liblkv.so (declared in include/lkv.h): host-side validation,
 // launch-geometry selection and dispatch to the gfx950 kernels.
+#include <math.h>
 #include <stdlib.h>
 
 #include <atomic>
 #include <mutex>
 
+#include "attn_kernels.h"
 #include "decode_kernels.h"
 #include "diag_kernels.h"
 #include "gather_kernels.h"
@@ -519,6 +521,133 @@ lkv_status scratch_for_current_device(char** out) {
     return LKV_OK;
 }
 
+// ---- full-attention layers
+
+lkv_status check_attn(const lkv_attn* A) {
+    if (!A) return LKV_E_NULL;
+    if (A->h_q < 1 || A->h_kv < 1 || A->h_q % A->h_kv != 0 || A->d < 1 || A->page < 1) return LKV_E_SHAPE;
+    if (!(A->scale > 0.f) || !isfinite(A->scale)) return LKV_E_SHAPE;
+    if (A->io_dtype != LKV_F32 && A->io_dtype != LKV_BF16) return LKV_E_DTYPE;
+    if (A->cache_dtype != A->io_dtype && !(A->cache_dtype == LKV_E4M3 && A->io_dtype == LKV_BF16)) return LKV_E_DTYPE;
+    if (A->d != 64 && A->d != 128 && !(A->d == 256 && A->io_dtype == LKV_BF16)) return LKV_E_UNSUPPORTED;
+    if (A->page < 16 || A->page > 1024 || (A->page & (A->page - 1)) != 0) return LKV_E_UNSUPPORTED;
+    return LKV_OK;
+}
+
+int kv_kind(const lkv_attn* A) {
+    return A->cache_dtype == LKV_E4M3 ? KV_E4M3 : A->cache_dtype == LKV_F32 ? KV_F32 : KV_BF16;
+}
+
+// token counts, and that indexes of rows and workgroups stay below 2^31
+lkv_status check_counts(const lkv_attn* A, int32_t n_req, int64_t n_tok) {
+    if (n_req < 0 || n_tok < 0) return LKV_E_SHAPE;
+    if (n_tok > INT32_MAX / A->h_q) return LKV_E_SHAPE;
+    if (((int64_t)n_req + n_tok * A->h_q / A->h_kv) > INT32_MAX / A->h_kv) return LKV_E_SHAPE;
+    return LKV_OK;
+}
+
+// rows of `heads` heads, `stride` elements apart
+lkv_status check_rows(const lkv_attn* A, const void* x, int64_t stride, int32_t heads) {
+    if (!x) return LKV_E_NULL;
+    if (stride < (int64_t)heads * A->d || stride > INT64_C(1) << 31) return LKV_E_SHAPE;
+    if (!aligned16(x) || stride * (A->io_dtype == LKV_BF16 ? 2 : 4) % 16 != 0) return LKV_E_ALIGN;
+    return LKV_OK;
+}
+
+lkv_status check_pages(const lkv_attn* A, const lkv_pages* P) {
+    if (!P) return LKV_E_NULL;
+    if (P->n_page < 0 || P->max_pages < 0 || P->max_pages > INT32_MAX / A->page) return LKV_E_SHAPE;
+    if (!P->len || (P->max_pages > 0 && !P->table)) return LKV_E_NULL;
+    if (P->n_page > 0) {
+        if (!P->k || !P->v) return LKV_E_NULL;
+        if (A->cache_dtype == LKV_E4M3 && (!P->k_exp || !P->v_exp)) return LKV_E_NULL;
+        if (!aligned16(P->k) || !aligned16(P->v)) return LKV_E_ALIGN;
+    }
+    return LKV_OK;
+}
+
+PagesArgs pages_args(const lkv_attn* A, const lkv_pages* P) {
+    PagesArgs g = {};
+    g.k = P->k;
+    g.v = P->v;
+    g.k_exp = P->k_exp;
+    g.v_exp = P->v_exp;
+    g.table = P->table;
+    g.len = P->len;
+    g.n_page = P->n_page;
+    g.max_pages = P->n_page > 0 ? P->max_pages : 0;  // without pages every context is empty
+    while ((1 << g.page_shift) < A->page) ++g.page_shift;
+    return g;
+}
+
+AttnArgs attn_args(const lkv_attn* A, const int32_t* cu, int32_t n_req, int64_t n_tok, const void* q, int64_t q_stride,
+                   void* o) {
+    AttnArgs a = {};
+    a.cu = cu;
+    a.n_req = n_req;
+    a.n_tok = n_tok;
+    a.q = q;
+    a.q_stride = q_stride;
+    a.o = o;
+    a.h_q = A->h_q;
+    a.h_kv = A->h_kv;
+    a.group = A->h_q / A->h_kv;
+    a.scale_log2 = A->scale * 1.4426950408889634f;
+    a.splits = 1;
+    const int rows = A->io_dtype == LKV_F32 ? ATTN_ROWS_F32 : ATTN_ROWS;
+    a.n_units = (int32_t)(n_req + (n_tok * a.group - 1) / rows);
+    return a;
+}
+
+// Parts of the key range of a paged call: enough workgroups for the 256 CUs, none below 256 keys
+int attn_splits(const lkv_attn* A, int32_t n_req, int64_t n_tok, int32_t max_pages) {
+    const int rows = A->io_dtype == LKV_F32 ? ATTN_ROWS_F32 : ATTN_ROWS;
+    const int64_t wgs = (n_req + (n_tok * (A->h_q / A->h_kv) - 1) / rows) * (int64_t)A->h_kv;
+    if (wgs >= 512) return 1;
+    int64_t s = (1024 + wgs - 1) / wgs;
+    const int64_t most = ((int64_t)max_pages * A->page + 255) / 256;
+    s = s < most ? s : most;
+    return (int)(s < 1 ? 1 : (s > 128 ? 128 : s));
+}
+
+struct AttnWs {
+    size_t o, ml, total;
+};
+AttnWs attn_ws(const lkv_attn* A, int64_t n_tok, int splits) {
+    AttnWs w = {};
+    if (splits <= 1) return w;
+    const size_t rows = (size_t)splits * n_tok * A->h_q;
+    w.ml = (rows * A->d * 4 + 255) & ~size_t(255);
+    w.total = w.ml + rows * 8;
+    return w;
+}
+
+lkv_status kv_move(const lkv_attn* A, const lkv_pages* P, const int32_t* cu, int32_t n_req, int64_t n_tok,
+                   const int32_t* pos, void* k, int64_t k_stride, void* v, int64_t v_stride, bool write, void* stream) {
+    lkv_status s = check_attn(A);
+    if (s == LKV_OK) s = check_counts(A, n_req, n_tok);
+    if (s == LKV_OK) s = check_pages(A, P);
+    if (s != LKV_OK || n_req == 0 || n_tok == 0) return s;
+    if (!cu) return LKV_E_NULL;
+    s = check_rows(A, k, k_stride, A->h_kv);
+    if (s == LKV_OK) s = check_rows(A, v, v_stride, A->h_kv);
+    if (s != LKV_OK) return s;
+    KvArgs a = {};
+    a.cu = cu;
+    a.n_req = n_req;
+    a.n_tok = n_tok;
+    a.pos = pos;
+    a.k = k;
+    a.v = v;
+    a.k_stride = k_stride;
+    a.v_stride = v_stride;
+    a.h_kv = A->h_kv;
+    a.d = A->d;
+    a.kind = kv_kind(A);
+    a.pg = pages_args(A, P);
+    return hip_status(write ? launch_kv_write(a, (hipStream_t)stream) : launch_kv_read(a, (hipStream_t)stream));
+}
+
 }  // namespace
 
 extern "C" {
@@ -758,6 +887,77 @@ lkv_status lkv_chunk_scan_sp_noalloc(const lkv_layer* L, const lkv_tokens* T, fl
     s = scratch_for_current_device(&ws);
     if (s != LKV_OK) return s;
     return chunk_scan_sp(L, T, scale, S_init, out, S_final, pieces, ws, kScratchBytes, stream);
+}
+
+lkv_status lkv_attn_prefill(const lkv_attn* A, const int32_t* cu, int32_t n_seq, int64_t n_tok, const void* q,
+                            int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride, void* o,
+                            void* stream) {
+    lkv_status s = check_attn(A);
+    if (s == LKV_OK) s = check_counts(A, n_seq, n_tok);
+    if (s != LKV_OK || n_seq == 0 || n_tok == 0) return s;
+    if (!cu || !o) return LKV_E_NULL;
+    s = check_rows(A, q, q_stride, A->h_q);
+    if (s == LKV_OK) s = check_rows(A, k, k_stride, A->h_kv);
+    if (s == LKV_OK) s = check_rows(A, v, v_stride, A->h_kv);
+    if (s != LKV_OK) return s;
+    if (!aligned16(o)) return LKV_E_ALIGN;
+    AttnArgs a = attn_args(A, cu, n_seq, n_tok, q, q_stride, o);
+    a.k = k;
+    a.v = v;
+    a.k_stride = k_stride;
+    a.v_stride = v_stride;
+    hipStream_t st = (hipStream_t)stream;
+    return hip_status(A->io_dtype == LKV_F32 ? launch_attn_f32(A->d, false, a, st) : launch_attn(A->d, KV_BF16, false, a, st));
+}
+
+lkv_status lkv_kv_write(const lkv_attn* A, const lkv_pages* P, const int32_t* cu, int32_t n_req, int64_t n_tok,
+                        const int32_t* pos, const void* k, int64_t k_stride, const void* v, int64_t v_stride, void* stream) {
+    return kv_move(A, P, cu, n_req, n_tok, pos, const_cast<void*>(k), k_stride, const_cast<void*>(v), v_stride, true, stream);
+}
+
+lkv_status lkv_kv_read(const lkv_attn* A, const lkv_pages* P, const int32_t* cu, int32_t n_req, int64_t n_tok,
+                       const int32_t* pos, void* k, int64_t k_stride, void* v, int64_t v_stride, void* stream) {
+    return kv_move(A, P, cu, n_req, n_tok, pos, k, k_stride, v, v_stride, false, stream);
+}
+
+lkv_status lkv_attn_paged_workspace(const lkv_attn* A, int32_t n_req, int64_t n_tok, int32_t max_pages, size_t* bytes) {
+    if (!bytes) return LKV_E_NULL;
+    lkv_status s = check_attn(A);
+    if (s == LKV_OK) s = check_counts(A, n_req, n_tok);
+    if (s != LKV_OK) return s;
+    if (max_pages < 0 || max_pages > INT32_MAX / A->page) return LKV_E_SHAPE;
+    *bytes = n_req == 0 || n_tok == 0 ? 0 : attn_ws(A, n_tok, attn_splits(A, n_req, n_tok, max_pages)).total;
+    return LKV_OK;
+}
+
+lkv_status lkv_attn_paged(const lkv_attn* A, const lkv_pages* P, const int32_t* cu, int32_t n_req, int64_t n_tok,
+                          const int32_t* pos, const void* q, int64_t q_stride, void* o, void* ws, size_t ws_bytes,
+                          void* stream) {
+    lkv_status s = check_attn(A);
+    if (s == LKV_OK) s = check_counts(A, n_req, n_tok);
+    if (s == LKV_OK) s = check_pages(A, P);
+    if (s != LKV_OK || n_req == 0 || n_tok == 0) return s;
+    if (!cu || !o) return LKV_E_NULL;
+    s = check_rows(A, q, q_stride, A->h_q);
+    if (s != LKV_OK) return s;
+    if (!aligned16(o)) return LKV_E_ALIGN;
+    AttnArgs a = attn_args(A, cu, n_req, n_tok, q, q_stride, o);
+    a.pos = pos;
+    a.pg = pages_args(A, P);
+    a.splits = attn_splits(A, n_req, n_tok, P->max_pages);
+    const AttnWs w = attn_ws(A, n_tok, a.splits);
+    if (w.total > 0) {
+        if (!ws) return LKV_E_NULL;
+        if (((uintptr_t)ws & 255u) != 0) return LKV_E_ALIGN;
+        if (ws_bytes < w.total) return LKV_E_SHAPE;
+        a.part_o = reinterpret_cast<float*>(ws);
+        a.part_ml = reinterpret_cast<float*>(reinterpret_cast<char*>(ws) + w.ml);
+    }
+    hipStream_t st = (hipStream_t)stream;
+    const bool f32 = A->io_dtype == LKV_F32;
+    s = hip_status(f32 ? launch_attn_f32(A->d, true, a, st) : launch_attn(A->d, kv_kind(A), true, a, st));
+    if (s != LKV_OK || a.splits == 1) return s;
+    return hip_status(launch_attn_join(A->d, f32, a, st));
 }
 
 }  // extern "C"

@@ -18,7 +18,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "liblkv.so")
 
 GDN, SSD = 0, 1
-F32, BF16 = 0, 1
+F32, BF16, E4M3 = 0, 1, 2
 
 _STATUS = {0: "LKV_OK", 1: "LKV_E_NULL", 2: "LKV_E_SHAPE", 3: "LKV_E_DTYPE", 4: "LKV_E_ALIGN",
            5: "LKV_E_UNSUPPORTED", 6: "LKV_E_WORKSPACE", 7: "LKV_E_HIP"}
@@ -45,6 +45,17 @@ class Tokens(ctypes.Structure):
                 ("g", ctypes.c_void_p), ("beta", ctypes.c_void_p), ("A", ctypes.c_void_p)]
 
 
+class Attn(ctypes.Structure):
+    _fields_ = [("h_q", ctypes.c_int32), ("h_kv", ctypes.c_int32), ("d", ctypes.c_int32), ("page", ctypes.c_int32),
+                ("io_dtype", ctypes.c_int32), ("cache_dtype", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
+class Pages(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_exp", ctypes.c_void_p), ("v_exp", ctypes.c_void_p),
+                ("n_page", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("table", ctypes.c_void_p),
+                ("len", ctypes.c_void_p)]
+
+
 _lib = None
 _lock = threading.Lock()
 EXPORTS = ("lkv_abi_version", "lkv_status_string", "lkv_last_hip_error", "lkv_block_summary",
@@ -52,7 +63,8 @@ EXPORTS = ("lkv_abi_version", "lkv_status_string", "lkv_last_hip_error", "lkv_bl
            "lkv_gdn_decode", "lkv_ssd_decode", "lkv_gather_selected", "lkv_init_single_bf16",
            "lkv_init_compose_bf16", "lkv_round_bf16", "lkv_stage_rows", "lkv_state_rel_error",
            "lkv_chunk_scan_from_pool", "lkv_set_wait_limit", "lkv_chunk_scan_sp_workspace",
-           "lkv_chunk_scan_sp", "lkv_chunk_scan_sp_noalloc")
+           "lkv_chunk_scan_sp", "lkv_chunk_scan_sp_noalloc", "lkv_attn_prefill", "lkv_kv_write", "lkv_kv_read",
+           "lkv_attn_paged_workspace", "lkv_attn_paged")
 
 
 def load() -> ctypes.CDLL:
@@ -91,10 +103,17 @@ def load() -> ctypes.CDLL:
             lib.lkv_stage_rows.argtypes = [vp, vp, vp, i32, ctypes.c_int64, vp]
             lib.lkv_state_rel_error.argtypes = [vp, vp, i32, ctypes.c_int64, i32, vp, vp, vp, vp]
             lib.lkv_chunk_scan_from_pool.argtypes = [LP, TP, f32, vp, i32, i32, vp, vp, vp, vp]
+            i64, AP, PP = ctypes.c_int64, ctypes.POINTER(Attn), ctypes.POINTER(Pages)
+            lib.lkv_attn_prefill.argtypes = [AP, vp, i32, i64, vp, i64, vp, i64, vp, i64, vp, vp]
+            lib.lkv_kv_write.argtypes = [AP, PP, vp, i32, i64, vp, vp, i64, vp, i64, vp]
+            lib.lkv_kv_read.argtypes = [AP, PP, vp, i32, i64, vp, vp, i64, vp, i64, vp]
+            lib.lkv_attn_paged_workspace.argtypes = [AP, i32, i64, i32, ctypes.POINTER(ctypes.c_size_t)]
+            lib.lkv_attn_paged.argtypes = [AP, PP, vp, i32, i64, vp, vp, i64, vp, vp, ctypes.c_size_t, vp]
             for f in ("lkv_block_summary", "lkv_init_single", "lkv_init_compose", "lkv_gdn_chunk_scan",
                       "lkv_ssd_chunk_scan", "lkv_gdn_decode", "lkv_ssd_decode", "lkv_gather_selected",
                       "lkv_init_single_bf16", "lkv_init_compose_bf16", "lkv_round_bf16", "lkv_stage_rows",
-                      "lkv_state_rel_error", "lkv_chunk_scan_from_pool"):
+                      "lkv_state_rel_error", "lkv_chunk_scan_from_pool", "lkv_attn_prefill", "lkv_kv_write", "lkv_kv_read",
+                      "lkv_attn_paged_workspace", "lkv_attn_paged"):
                 getattr(lib, f).restype = ctypes.c_int
             _lib = lib
     return _lib
@@ -308,3 +327,131 @@ def chunk_scan_sp_noalloc(layer: Layer, online: Tokens, scale: float, S_init: Op
     _check(load().lkv_chunk_scan_sp_noalloc(ctypes.byref(layer), ctypes.byref(online), float(scale), _ptr(S_init),
                                             _ptr(out), _ptr(S_final), int(pieces), _stream(stream)),
            "lkv_chunk_scan_sp_noalloc")
+
+
+# ---- full-attention layers ------------------------------------------------
+
+def make_attn(h_q: int, h_kv: int, d: int, scale: Optional[float] = None, page: int = 64,
+              io_dtype: torch.dtype = torch.bfloat16, cache_dtype: Optional[torch.dtype] = None) -> Attn:
+    """Geometry of one full-attention layer.  ``scale`` defaults to ``d ** -0.5``; ``cache_dtype`` to
+    ``io_dtype``, and is ``torch.float8_e4m3fn`` for a quantised cache."""
+    cache = dtype_code(io_dtype) if cache_dtype is None else (
+        E4M3 if cache_dtype == torch.float8_e4m3fn else dtype_code(cache_dtype))
+    a = Attn(h_q, h_kv, d, page, dtype_code(io_dtype), cache, d ** -0.5 if scale is None else scale)
+    a._io = io_dtype
+    a._cache = {F32: torch.float32, BF16: torch.bfloat16, E4M3: torch.float8_e4m3fn}[cache]
+    return a
+
+
+def _index(t: torch.Tensor, what: str, rows: int, dim: int = 1):
+    if t.dtype != torch.int32 or t.dim() != dim or t.shape[0] < rows:
+        raise ValueError(f"{what}: int32 of {dim} dimension(s) and at least {rows} rows expected")
+    _here(t, what)
+    return _ptr(t)
+
+
+def _here(t: torch.Tensor, what: str):
+    if t.get_device() != (_raw_device() if _raw_device is not None else torch.cuda.current_device()):
+        raise ValueError(f"{what}: not on the current GPU")
+
+
+def _rows(a: Attn, t: torch.Tensor, n_tok: int, heads: int, what: str):
+    """Pointer and token stride of a [n_tok, heads, d] tensor whose tokens may lie apart."""
+    d = a.d
+    if t.dim() != 3 or t.shape[0] < n_tok or t.shape[1] != heads or t.shape[2] != d or t.dtype != a._io:
+        raise ValueError(f"{what}: {a._io} [{n_tok}, {heads}, {d}] expected, got {t.dtype} {tuple(t.shape)}")
+    s0, s1, s2 = t.stride()
+    if s2 != 1 or (heads > 1 and s1 != d):
+        raise ValueError(f"{what}: a token's heads must be contiguous")
+    _here(t, what)
+    return t.data_ptr(), (s0 if t.shape[0] > 1 else heads * d)
+
+
+def make_pages(attn: Attn, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, length: torch.Tensor,
+               k_exp: Optional[torch.Tensor] = None, v_exp: Optional[torch.Tensor] = None) -> Pages:
+    """Paged cache: ``k`` and ``v`` [n_page, h_kv, page, d] (with ``k_exp``, ``v_exp`` uint8 [n_page, h_kv,
+    page] for e4m3), ``table`` int32 [n_req, max_pages], ``length`` int32 [n_req], all on the GPU."""
+    shape = (k.shape[0], attn.h_kv, attn.page, attn.d)
+    for x, what in ((k, "k"), (v, "v")):
+        if tuple(x.shape) != shape or x.dtype != attn._cache:
+            raise ValueError(f"{what}: {attn._cache} {shape} expected, got {x.dtype} {tuple(x.shape)}")
+    exps = attn.cache_dtype == E4M3
+    for x, what in ((k_exp, "k_exp"), (v_exp, "v_exp")):
+        if exps != (x is not None):
+            raise ValueError(f"{what}: given with an e4m3 cache, and only then")
+        if exps and (tuple(x.shape) != shape[:3] or x.dtype != torch.uint8):
+            raise ValueError(f"{what}: uint8 {shape[:3]} expected")
+    for x, what in ((k, "k"), (v, "v"), (k_exp, "k_exp"), (v_exp, "v_exp")):
+        if x is not None:
+            _here(x, what)
+    p = Pages()
+    p.k, p.v, p.k_exp, p.v_exp = _ptr(k), _ptr(v), _ptr(k_exp), _ptr(v_exp)
+    p.table = _index(table, "table", 0, 2)
+    p.len = _index(length, "length", table.shape[0])
+    p.n_page, p.max_pages = int(k.shape[0]), int(table.shape[1])
+    p._keep = (k, v, table, length, k_exp, v_exp)
+    p._n_req, p._attn = int(table.shape[0]), attn
+    return p
+
+
+def _paged(attn: Attn, pages: Pages, cu: torch.Tensor, n_tok: int, pos: Optional[torch.Tensor]):
+    n_req = int(cu.shape[0]) - 1
+    own = pages._attn
+    if own is not attn and (own.h_kv, own.page, own.d, own.cache_dtype) != (attn.h_kv, attn.page, attn.d, attn.cache_dtype):
+        raise ValueError("pages: made for another layer geometry")
+    if n_req > pages._n_req:
+        raise ValueError("pages: fewer rows in the table than requests")
+    return _index(cu, "cu", 1), n_req, None if pos is None else _index(pos, "pos", n_tok)
+
+
+def attn_prefill(attn: Attn, cu: torch.Tensor, n_tok: int, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+                 o: torch.Tensor, stream=None) -> None:
+    """Causal attention over the packed sequences ``cu``.  q, o [n_tok, h_q, d], k, v [n_tok, h_kv, d]; the
+    tokens of q, k and v may lie apart (views of one projection's output), o is dense."""
+    qp, qs = _rows(attn, q, n_tok, attn.h_q, "q")
+    kp, ks = _rows(attn, k, n_tok, attn.h_kv, "k")
+    vp, vs = _rows(attn, v, n_tok, attn.h_kv, "v")
+    _rows(attn, o, n_tok, attn.h_q, "o")
+    _check(load().lkv_attn_prefill(attn, _index(cu, "cu", 1), int(cu.shape[0]) - 1, n_tok, qp, qs, kp, ks, vp, vs,
+                                   _ptr(o), _stream(stream)), "lkv_attn_prefill")
+
+
+def kv_write(attn: Attn, pages: Pages, cu: torch.Tensor, n_tok: int, k: torch.Tensor, v: torch.Tensor,
+             pos: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Write tokens' k and v [n_tok, h_kv, d] to positions ``pos`` (default: the last) of their requests' contexts."""
+    cup, n_req, posp = _paged(attn, pages, cu, n_tok, pos)
+    kp, ks = _rows(attn, k, n_tok, attn.h_kv, "k")
+    vp, vs = _rows(attn, v, n_tok, attn.h_kv, "v")
+    _check(load().lkv_kv_write(attn, pages, cup, n_req, n_tok, posp, kp, ks, vp, vs, _stream(stream)), "lkv_kv_write")
+
+
+def kv_read(attn: Attn, pages: Pages, cu: torch.Tensor, n_tok: int, k: torch.Tensor, v: torch.Tensor,
+            pos: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Read the rows at positions ``pos`` (default: the last) of the requests' contexts into k and v."""
+    cup, n_req, posp = _paged(attn, pages, cu, n_tok, pos)
+    kp, ks = _rows(attn, k, n_tok, attn.h_kv, "k")
+    vp, vs = _rows(attn, v, n_tok, attn.h_kv, "v")
+    _check(load().lkv_kv_read(attn, pages, cup, n_req, n_tok, posp, kp, ks, vp, vs, _stream(stream)), "lkv_kv_read")
+
+
+def attn_paged_workspace(attn: Attn, n_req: int, n_tok: int, max_pages: int) -> int:
+    """Workspace bytes of attn_paged."""
+    n = ctypes.c_size_t(0)
+    _check(load().lkv_attn_paged_workspace(attn, int(n_req), int(n_tok), int(max_pages), ctypes.byref(n)),
+           "lkv_attn_paged_workspace")
+    return int(n.value)
+
+
+def attn_paged(attn: Attn, pages: Pages, cu: torch.Tensor, n_tok: int, q: torch.Tensor, o: torch.Tensor,
+               ws: Optional[torch.Tensor], pos: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Attention of new tokens q [n_tok, h_q, d] over the paged cache, at positions ``pos`` (default: the
+    last of each context); ``ws`` is a device workspace tensor (None or empty if it needs 0 bytes)."""
+    cup, n_req, posp = _paged(attn, pages, cu, n_tok, pos)
+    qp, qs = _rows(attn, q, n_tok, attn.h_q, "q")
+    _rows(attn, o, n_tok, attn.h_q, "o")
+    ws_bytes = 0
+    if ws is not None:
+        ws_bytes = ws.numel() * ws.element_size()
+        _here(ws, "ws")
+    _check(load().lkv_attn_paged(attn, pages, cup, n_req, n_tok, posp, qp, qs, _ptr(o),
+                                 _ptr(ws) if ws_bytes else None, ws_bytes, _stream(stream)), "lkv_attn_paged")
