@@ -388,8 +388,8 @@ lkv_status lkv_state_rel_error(const float* S, const float* S_ref, int32_t n_sli
  * sees is infinite or NaN, that element of its output is not finite.
  *
  * Token arrays have rows [heads, d] `stride` elements apart (a multiple of 16
- * bytes, at least heads * d), so q, k and v may be views of one projection's
- * output; o is dense.  cu: device int32 [n_req+1], cu[0] = 0, non-decreasing;
+ * bytes, at least heads * d, at most 2^22), so q, k and v may be views of one
+ * projection's output; o is dense.  cu: device int32 [n_req+1], cu[0] = 0, non-decreasing;
  * n_tok: host bound of cu[n_req].  Rows from cu[n_req] on are not touched, so
  * a padded batch (a captured graph's) may pass its capacity. */
 typedef struct {

@@ -549,7 +549,8 @@ lkv_status check_counts(const lkv_attn* A, int32_t n_req, int64_t n_tok) {
 // rows of `heads` heads, `stride` elements apart
 lkv_status check_rows(const lkv_attn* A, const void* x, int64_t stride, int32_t heads) {
     if (!x) return LKV_E_NULL;
-    if (stride < (int64_t)heads * A->d || stride > INT64_C(1) << 31) return LKV_E_SHAPE;
+    if (stride < (int64_t)heads * A->d) return LKV_E_SHAPE;
+    if (stride > 1 << 22) return LKV_E_UNSUPPORTED;  // a key tile's byte offsets are 32-bit
     if (!aligned16(x) || stride * (A->io_dtype == LKV_BF16 ? 2 : 4) % 16 != 0) return LKV_E_ALIGN;
     return LKV_OK;
 }

@@ -66,6 +66,7 @@ def test_prefill_arguments():
     assert [_prefill(a, **{x: P + 8}) for x in ("q", "k", "v", "o")] == [ALIGN] * 4
     assert [_prefill(a, **{x: 128}) for x in ("qs", "ks", "vs")] == [SHAPE] * 3  # rows would overlap
     assert [_prefill(a, **{x: 1028}) for x in ("qs", "ks", "vs")] == [ALIGN] * 3
+    assert [_prefill(a, **{x: (1 << 22) + 8}) for x in ("qs", "ks", "vs")] == [UNSUPPORTED] * 3
 
 
 def test_paged_arguments():
