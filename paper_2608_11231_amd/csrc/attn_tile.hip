@@ -9,16 +9,24 @@
 // fragment is read from LDS with transposing reads of just those keys.
 //
 // The scores, the softmax's statistics and O are fp32; the probabilities are rounded to bf16
-// for the product (2^-9 of each, below the outputs' own rounding).
+// for the product (2^-8 of each at most, as the outputs are).
+//
+// Power bounds the large calls (4 waves of 32 rows, two workgroups per CU: the clock falls to 2.0
+// GHz with the matrix cores half busy): a 32K prompt of 32/8 heads of 128 takes 8.3 ms, 1.06
+// PFLOP/s.  Measured beside it and not better: the next tile's scores formed in between softmax
+// and product (8.3), eight waves that share a tile (8.4), three waves per SIMD on tiles of 32 keys
+// (8.2; 32 ragged blocks 490 against 460 us), keys staged through registers (8.0 with eight
+// waves, blocks 470, but paged keys 6.2 against 4.7 ms), 64 rows per wave with one wave per SIMD
+// (10.0: each fragment read serves two products, but nothing hides the LDS and barrier waits).
 #include "attn_device.h"
 
 namespace lkv {
 
 namespace {
 
-constexpr int NW = 4;            // waves
-constexpr int BM = ATTN_ROWS;    // rows
-static_assert(BM == 32 * NW, "a wave owns 32 rows");
+#define INLINE __attribute__((always_inline))  // lambdas over register arrays
+
+constexpr int NW = 4;  // waves
 
 // Position of 16-byte chunk c of row r in a tile of bf16 rows in LDS (in chunks).  K fragments
 // are read as one chunk of 32 consecutive rows, V fragments as 4 adjacent chunks of 4 rows, twice:
@@ -58,6 +66,16 @@ __device__ __forceinline__ u32x4 one_bits(uint32_t b) {
     return x;
 }
 
+// Maximum and sum over the wave's two halves
+__device__ __forceinline__ float half_max(float x) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
+    return fmaxf(__builtin_bit_cast(float, (uint32_t)r[0]), __builtin_bit_cast(float, (uint32_t)r[1]));
+}
+__device__ __forceinline__ float half_sum(float x) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
+    return __builtin_bit_cast(float, (uint32_t)r[0]) + __builtin_bit_cast(float, (uint32_t)r[1]);
+}
+
 // Reads at byte offsets in LDS
 typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
 typedef __attribute__((address_space(3))) lds_i16x4 lds_tr_t;
@@ -73,70 +91,58 @@ __device__ __forceinline__ bf16x4 tr_read(uint32_t at) {
 
 }  // namespace
 
-// Staging of key tiles: thread's 16-byte pieces of the K and V rows, K and V alike.  Rows past the last
-// key seen repeat it.  bf16 rows go from memory straight to LDS (a wave's 64 pieces land in
+// Staging of one side's tiles (keys, or values): the thread's 16-byte pieces of the rows.  Rows past the
+// last key seen repeat it.  bf16 rows go from memory straight to LDS (a wave's 64 pieces land in
 // consecutive chunks, so each lane fetches the piece that belongs to its chunk); e4m3 rows pass
 // through registers, where they become bf16.
-template <int D, int KIND, bool PAGED, int BN>
+template <int D, int KIND, bool PAGED, int BN, bool V>
 struct Stage {
-    static constexpr int C = D / 8;                       // chunks of a bf16 row
+    static constexpr int C = D / 8;                         // chunks of a bf16 row
     static constexpr int U = KIND == KV_E4M3 ? D / 16 : C;  // pieces of a stored row
     static constexpr int PER = BN * U / (64 * NW);
-    static constexpr int EB = KIND == KV_E4M3 ? 1 : 2;
     static_assert(64 / U <= 16, "a wave's rows of one piece are in one page");
     const AttnArgs& p;
     const AttnUnit& w;
+    const char* base;  // the pool; packed sequences: the next tile's first row
+    int64_t stride;    // elements between rows, packed sequences
     int hk, end, tid, lane, wave;
-    int k_off[PER], v_off[PER];  // bytes from the tile's (its page's) first row, full tiles
-    int ids, ids_next;           // lane i: page of keys 16 i .. of the next tile, and of the one behind it
-    u32x4 kr[PER], vr[PER];      // e4m3 pieces on their way
-    float ks[PER], vs[PER];
+    int off[PER];       // bytes from the tile's (its page's) first row, full tiles
+    int ids, ids_next;  // lane i: page of keys 16 i .. of the next tile to fetch, and of the one behind it
+    u32x4 r[PER];       // e4m3 pieces on their way
+    float scale[PER];
     bool bad_page = false;
 
     __device__ __forceinline__ Stage(const AttnArgs& p_, const AttnUnit& w_, int hk_, int end_, int tid_)
-        : p(p_), w(w_), hk(hk_), end(end_), tid(tid_), lane(tid_ & 63), wave(__builtin_amdgcn_readfirstlane(tid_ >> 6)) {
+        : p(p_), w(w_), base(reinterpret_cast<const char*>(PAGED ? (V ? p_.pg.v : p_.pg.k) : (V ? p_.v : p_.k))),
+          stride(V ? p_.v_stride : p_.k_stride), hk(hk_), end(end_), tid(tid_), lane(tid_ & 63), wave(__builtin_amdgcn_readfirstlane(tid_ >> 6)) {
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            const int r = row(i);
-            if (PAGED) {
-                const int slot = r & ((1 << p.pg.page_shift) - 1);
-                k_off[i] = (slot * U + piece(i, false)) * 16;
-                v_off[i] = (slot * U + piece(i, true)) * 16;
-            } else {
-                k_off[i] = r * (int)p.k_stride * 2 + piece(i, false) * 16;
-                v_off[i] = r * (int)p.v_stride * 2 + piece(i, true) * 16;
-            }
+            const int x = tid + i * 64 * NW, row = x / U, c = x % U;
+            // the permutation of a row's chunks is its own inverse
+            const int piece = KIND == KV_E4M3 ? c : (V ? v_chunk<D>(row, c) : k_chunk<D>(row, c)) - row * C;
+            off[i] = PAGED ? ((row & ((1 << p.pg.page_shift) - 1)) * U + piece) * 16 : row * (int)stride * 2 + piece * 16;
         }
     }
     __device__ __forceinline__ int row(int i) const { return (tid + i * 64 * NW) / U; }
-    // the piece of its row that this thread fetches
-    __device__ __forceinline__ int piece(int i, bool v) const {
-        const int x = tid + i * 64 * NW, r = x / U, c = x % U;
-        if (KIND == KV_E4M3) return c;
-        return (v ? v_chunk<D>(r, c) : k_chunk<D>(r, c)) - r * C;  // the permutation is its own inverse
-    }
-    // page ids of the tile at j0
     __device__ __forceinline__ int load_ids(int j0) const {
         if (!PAGED) return 0;
         const int j = min(j0 + 16 * (lane & (BN / 16 - 1)), end - 1);
         return p.pg.table[(int64_t)w.r * p.pg.max_pages + (j >> p.pg.page_shift)];
     }
     __device__ __forceinline__ void begin(int j0) {
+        if (!PAGED) base += ((w.t0 + j0) * stride + (int64_t)hk * D) * 2;
         ids = load_ids(j0);
         ids_next = load_ids(j0 + BN);
     }
-    __device__ __forceinline__ const char* at(const void* base, int64_t row, int64_t bytes) const {
-        return reinterpret_cast<const char*>(base) + row * bytes;
-    }
-    // starts the fetch of the tile at j0
-    __device__ __forceinline__ void fetch(int j0, u32x4* sk, u32x4* sv) {
+    // starts the fetch of the tile at j0; tiles are fetched in order
+    __device__ __forceinline__ void fetch(int j0, u32x4* lds) {
         const bool full = j0 + BN <= end;
         const int mask = (1 << p.pg.page_shift) - 1;
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            const char *kb, *vb;
-            int ko = k_off[i], vo = v_off[i];
+            int o = off[i];
             int64_t first = 0;
+            const char* b = base;
             if (PAGED) {
                 const int r0 = (wave * 64 + i * 64 * NW) / U;  // the wave's first row: its rows are in one page
                 int page = __builtin_amdgcn_readlane(ids, r0 / 16);
@@ -144,55 +150,36 @@ struct Stage {
                 bad_page |= !ok;
                 page = ok ? page : 0;
                 first = ((int64_t)page * p.h_kv + hk) << p.pg.page_shift;
-                if (full) {
-                    first += j0 & mask;
-                } else {
-                    const int move = (min(j0 + row(i), end - 1) & mask) - (row(i) & mask);
-                    ko += move * U * 16;
-                    vo += move * U * 16;
-                }
-                kb = at(p.pg.k, first, U * 16);
-                vb = at(p.pg.v, first, U * 16);
+                if (full) first += j0 & mask;
+                else o += ((min(j0 + row(i), end - 1) & mask) - (row(i) & mask)) * U * 16;
+                b += first * (U * 16);
             } else {
-                kb = at(p.k, (w.t0 + j0) * p.k_stride + (int64_t)hk * D, 2);
-                vb = at(p.v, (w.t0 + j0) * p.v_stride + (int64_t)hk * D, 2);
-                if (!full) {
-                    const int move = min(row(i), end - 1 - j0) - row(i);
-                    ko += move * (int)p.k_stride * 2;
-                    vo += move * (int)p.v_stride * 2;
-                }
+                if (!full) o += (min(row(i), end - 1 - j0) - row(i)) * (int)stride * 2;
             }
             if constexpr (KIND == KV_E4M3) {
-                kr[i] = *reinterpret_cast<const u32x4*>(kb + (uint32_t)ko);
-                vr[i] = *reinterpret_cast<const u32x4*>(vb + (uint32_t)vo);
-                ks[i] = exp_scale(p.pg.k_exp[first + (uint32_t)ko / (16 * U)]);
-                vs[i] = exp_scale(p.pg.v_exp[first + (uint32_t)vo / (16 * U)]);
+                r[i] = *reinterpret_cast<const u32x4*>(b + (uint32_t)o);
+                scale[i] = exp_scale((V ? p.pg.v_exp : p.pg.k_exp)[first + (uint32_t)o / (16 * U)]);
             } else {
                 typedef __attribute__((address_space(1))) const void global_t;
                 typedef __attribute__((address_space(3))) void lds_t;
-                const int x = wave * 64 + i * 64 * NW;
-                __builtin_amdgcn_global_load_lds((global_t*)(kb + (uint32_t)ko), (lds_t*)(sk + x), 16, 0, 0);
-                __builtin_amdgcn_global_load_lds((global_t*)(vb + (uint32_t)vo), (lds_t*)(sv + x), 16, 0, 0);
+                __builtin_amdgcn_global_load_lds((global_t*)(b + (uint32_t)o), (lds_t*)(lds + wave * 64 + i * 64 * NW), 16, 0, 0);
             }
         }
+        if (!PAGED) base += BN * stride * 2;
         ids = ids_next;
         ids_next = load_ids(j0 + 2 * BN);
     }
     // e4m3: the fetched tile into LDS
-    __device__ __forceinline__ void commit(u32x4* sk, u32x4* sv) {
+    __device__ __forceinline__ void commit(u32x4* lds) {
         if constexpr (KIND == KV_E4M3) {
 #pragma unroll
             for (int i = 0; i < PER; ++i) {
-                const int x = tid + i * 64 * NW, r = x / U, c = x % U;
+                const int x = tid + i * 64 * NW, row = x / U, c = x % U;
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    sk[k_chunk<D>(r, 2 * c + e)] =
-                        u32x4{e4m3_pair(kr[i][2 * e], ks[i], false), e4m3_pair(kr[i][2 * e], ks[i], true),
-                              e4m3_pair(kr[i][2 * e + 1], ks[i], false), e4m3_pair(kr[i][2 * e + 1], ks[i], true)};
-                    sv[v_chunk<D>(r, 2 * c + e)] =
-                        u32x4{e4m3_pair(vr[i][2 * e], vs[i], false), e4m3_pair(vr[i][2 * e], vs[i], true),
-                              e4m3_pair(vr[i][2 * e + 1], vs[i], false), e4m3_pair(vr[i][2 * e + 1], vs[i], true)};
-                }
+                for (int e = 0; e < 2; ++e)
+                    lds[V ? v_chunk<D>(row, 2 * c + e) : k_chunk<D>(row, 2 * c + e)] =
+                        u32x4{e4m3_pair(r[i][2 * e], scale[i], false), e4m3_pair(r[i][2 * e], scale[i], true),
+                              e4m3_pair(r[i][2 * e + 1], scale[i], false), e4m3_pair(r[i][2 * e + 1], scale[i], true)};
             }
         }
     }
@@ -202,7 +189,8 @@ template <int D, int KIND, bool PAGED>
 __global__ __launch_bounds__(64 * NW, 2) void attn_tile_kernel(AttnArgs p) {
     constexpr int BN = D == 256 ? 32 : 64;  // keys of a tile
     constexpr int NT = BN / 32, NS = D / 16, ND = D / 32, C = D / 8;
-    constexpr int CHUNKS = BN * C;
+    constexpr int CHUNKS = BN * C, BM = ATTN_ROWS;
+    static_assert(BM == 32 * NW, "a wave owns 32 rows");
     __shared__ __align__(512) u32x4 sk[2 * CHUNKS], sv[2 * CHUNKS];  // the fragments' offsets are combined by exclusive or
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int col = lane & 31, h = lane >> 5;
@@ -216,44 +204,48 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_tile_kernel(AttnArgs p) {
     if (w.r < 0) return;
     const int len = PAGED ? attn_len(p.pg, w.r) : w.n;
     const AttnRow row = attn_row<PAGED>(p, w, w.row0 + 32 * wave + col, hk, len);
-
-    // keys that some row of the workgroup sees, that all of its rows see, and that some row of the wave sees
+    const bool sees = row.kind == ROW_SEES;
+    const int my_pos = sees ? row.pos : 0x7fffffff;
+    // keys that some row of the workgroup sees, and that all of its rows see
     __shared__ int s_end[NW], s_all[NW];
-    const int sees = row.kind == ROW_SEES ? row.pos + 1 : 0;
-    const int wave_end = wave_max_int(sees);
-    const int wave_all = wave_min_int(row.kind == ROW_SEES ? sees : 0x7fffffff);
-    if (lane == 0) s_end[wave] = wave_end, s_all[wave] = wave_all;
+    int end = wave_max_int(sees ? row.pos + 1 : 0), all = wave_min_int(sees ? row.pos + 1 : 0x7fffffff);
+    if (lane == 0) s_end[wave] = end, s_all[wave] = all;
     __syncthreads();
-    int end = 0, all = 0x7fffffff;
 #pragma unroll
     for (int i = 0; i < NW; ++i) end = max(end, s_end[i]), all = min(all, s_all[i]);
     end = __builtin_amdgcn_readfirstlane(end);
     all = __builtin_amdgcn_readfirstlane(all);
     const KeyRange range = key_range<BN>(end, PAGED ? p.splits : 1, split);
 
-    Stage<D, KIND, PAGED, BN> stage(p, w, hk, end, tid);
-    if (range.from < range.to) {
-        stage.begin(range.from);
-        stage.fetch(range.from, sk, sv);
+    Stage<D, KIND, PAGED, BN, false> keys(p, w, hk, end, tid);
+    Stage<D, KIND, PAGED, BN, true> vals(p, w, hk, end, tid);
+    const int tiles = (range.to - range.from + BN - 1) / BN;
+    const int clear = min(max(all - range.from, 0) / BN, tiles);  // that every row of the workgroup sees whole
+    auto start = [&](int j) INLINE { return range.from + j * BN; };
+    int b0 = 0, b1 = CHUNKS * 16;  // buffers of the tile at hand and of the next one
+    auto k_buf = [&](int o) INLINE { return reinterpret_cast<u32x4*>(reinterpret_cast<char*>(sk) + o); };
+    auto v_buf = [&](int o) INLINE { return reinterpret_cast<u32x4*>(reinterpret_cast<char*>(sv) + o); };
+    if (tiles > 0) {
+        keys.begin(range.from);
+        vals.begin(range.from);
+        keys.fetch(range.from, sk);
+        vals.fetch(range.from, sv);
     }
 
     bf16x8 qf[NS];
+    const bf16* q = reinterpret_cast<const bf16*>(p.q) + row.tok * p.q_stride + (int64_t)row.head * D;
 #pragma unroll
-    for (int s = 0; s < NS; ++s) qf[s] = bf16x8{};
-    if (row.kind != ROW_NONE) {
-        const bf16* q = reinterpret_cast<const bf16*>(p.q) + row.tok * p.q_stride + (int64_t)row.head * D;
-#pragma unroll
-        for (int s = 0; s < NS; ++s) qf[s] = *reinterpret_cast<const bf16x8*>(q + 16 * s + 8 * h);
-    }
-
+    for (int s = 0; s < NS; ++s) qf[s] = row.kind == ROW_NONE ? bf16x8{} : *reinterpret_cast<const bf16x8*>(q + 16 * s + 8 * h);
     f32x16 ot[ND];
 #pragma unroll
     for (int t = 0; t < ND; ++t)
 #pragma unroll
         for (int i = 0; i < 16; ++i) ot[t][i] = 0.f;
-    float m = -INFINITY, l = 0.f;  // running maximum (scaled, base 2; see below) and this half's sum
-    const int my_pos = row.kind == ROW_SEES ? row.pos : 0x7fffffff;
-    stage.commit(sk, sv);
+    float m = -INFINITY, l = 0.f;  // reference of the exponents (base 2, see below) and this half's sum
+    if (tiles > 0) {
+        keys.commit(sk);
+        vals.commit(sv);
+    }
 
     // Byte offsets of the lane's fragments; the chunks' permutation is an exclusive or, so the others are
     // one operation away.  V^T fragments: lane i of a group of 16 addresses key i / 4, columns 4 (i % 4)
@@ -262,39 +254,45 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_tile_kernel(AttnArgs p) {
     const uint32_t k_at = lds_offset(sk) + 16 * k_chunk<D>(col, h);
     const uint32_t v_at = lds_offset(sv) + 16 * v_chunk<D>(vrow, vcol) + 8 * (i16 & 1);
     constexpr int ROW = 2 * D;  // bytes
-    auto k_frag = [&](uint32_t at, int t, int s) { return frag_read((at ^ (32 * s & 255 & (ROW - 1))) + 32 * t * ROW + (32 * s & ~255 & (ROW - 1))); };
-    auto v_frag = [&](uint32_t at, int t, int s) {
-        const uint32_t x = (at ^ (64 * t & 255 & (ROW - 1))) + (64 * t & ~255 & (ROW - 1)) + 16 * s * ROW;
-        const bf16x4 a = tr_read(x), c = tr_read((x ^ 32) + 8 * ROW);
+    auto k_frag = [&](uint32_t at, int t, int s) INLINE { return frag_read((at ^ (32 * s & 255 & (ROW - 1))) + 32 * t * ROW + (32 * s & ~255 & (ROW - 1))); };
+    auto v_frag = [&](uint32_t at, int t, int s) INLINE {
+        const uint32_t x = at ^ (64 * t & 255 & (ROW - 1)), y = (64 * t & ~255 & (ROW - 1)) + 16 * s * ROW;
+        const bf16x4 a = tr_read(x + y), c = tr_read((x ^ 32) + y + 8 * ROW);
         return __builtin_shufflevector(a, c, 0, 1, 2, 3, 4, 5, 6, 7);
     };
 
-    auto tile = [&](auto masked_c, int j0, int buf) {
-        constexpr bool MASKED = decltype(masked_c)::value;
-        const uint32_t ck = k_at + buf * CHUNKS * 16, cv = v_at + buf * CHUNKS * 16;
+    // Tile j, whose keys and values are in the buffers at b0; the next one's are sent for.
+    auto tile = [&](bool masked, int j) INLINE {
+        const bool more = j + 1 < tiles;
+        if (more) {
+            keys.fetch(start(j + 1), k_buf(b1));
+            vals.fetch(start(j + 1), v_buf(b1));
+        }
         f32x16 st[NT];
+        __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) st[t][i] = 0.f;
 #pragma unroll
-            for (int s = 0; s < NS; ++s) st[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_frag(ck, t, s), qf[s], st[t], 0, 0, 0);
+            for (int s = 0; s < NS; ++s) st[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_frag(k_at + b0, t, s), qf[s], st[t], 0, 0, 0);
         }
-        if (MASKED) {
+        __builtin_amdgcn_s_setprio(0);
+        if (masked) {
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (j0 + 32 * t + 8 * (i >> 2) + 4 * h + (i & 3) > my_pos) st[t][i] = -INFINITY;
+                for (int e = 0; e < 16; ++e)
+                    if (start(j) + 32 * t + 8 * (e >> 2) + 4 * h + (e & 3) > my_pos) st[t][e] = -INFINITY;
         }
+        // The reference m need not be the maximum, only near it: it follows when it is exceeded by more
+        // than 8 (probabilities up to 2^8), which after the first tiles is rare, and else O stays as it is.
         float top = st[0][0];
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) top = fmaxf(top, st[t][i]);
-        top = fmaxf(top, __shfl_xor(top, 32)) * p.scale_log2;
-        // m need not be the maximum itself, only near it: it follows when it is exceeded by more than 8
-        // (probabilities up to 2^8), which after the first tiles is rare, and else O stays as it is
+            for (int e = 0; e < 16; ++e) top = fmaxf(top, st[t][e]);
+        top = half_max(top) * p.scale_log2;
         if (__any(!(top <= m + 8.f))) {
             const float m_new = fmaxf(m, top);
             const float scale = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - m_new);
@@ -303,100 +301,105 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_tile_kernel(AttnArgs p) {
 #pragma unroll
             for (int t = 0; t < ND; ++t)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) ot[t][i] *= scale;
+                for (int e = 0; e < 16; ++e) ot[t][e] *= scale;
         }
         const float m_use = m == -INFINITY ? 0.f : m;  // only scores of -inf so far
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
             bf16x8 pf[2];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(st[t][i], p.scale_log2, -m_use));
-                l += e;
-                st[t][i] = e;
-            }
+            for (int i = 0; i < 16; ++i) st[t][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[t][i], p.scale_log2, -m_use));
 #pragma unroll
-            for (int s = 0; s < 2; ++s)
-                pf[s] = __builtin_bit_cast(
-                    bf16x8, u32x4{pack_bf16x2(st[t][8 * s], st[t][8 * s + 1]), pack_bf16x2(st[t][8 * s + 2], st[t][8 * s + 3]),
-                                  pack_bf16x2(st[t][8 * s + 4], st[t][8 * s + 5]), pack_bf16x2(st[t][8 * s + 6], st[t][8 * s + 7])});
+            for (int s = 0; s < 2; ++s) {
+                u32x4 x;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    x[i] = pack_bf16x2(st[t][8 * s + 2 * i], st[t][8 * s + 2 * i + 1]);
+                    // the sum is of the rounded probabilities, as the product's is
+                    const bf16x2 ones{(bf16)1.f, (bf16)1.f};
+                    l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, (uint32_t)x[i]), ones, l, false);
+                }
+                pf[s] = __builtin_bit_cast(bf16x8, x);
+            }
+            __builtin_amdgcn_s_setprio(1);
 #pragma unroll
             for (int s = 0; s < 2; ++s)
 #pragma unroll
                 for (int d = 0; d < ND; ++d)
-                    ot[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_frag(cv, d, 2 * t + s), pf[s], ot[d], 0, 0, 0);
+                    ot[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_frag(v_at + b0, d, 2 * t + s), pf[s], ot[d], 0, 0, 0);
+            __builtin_amdgcn_s_setprio(0);
         }
+        if (more) {
+            keys.commit(k_buf(b1));
+            vals.commit(v_buf(b1));
+        }
+        const int x = b0;
+        b0 = b1, b1 = x;
     };
 
-    // Two buffers: one tile is fetched while the one before it is worked on, with one barrier per tile.
-    // Tiles that every row of the workgroup sees whole come first, without masks.
-    int j0 = range.from, buf = 0;
-    auto arrive = [&]() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
-    for (; j0 < range.to && j0 + BN <= all; j0 += BN, buf ^= 1) {
-        arrive();
-        const bool more = j0 + BN < range.to;
-        if (more) stage.fetch(j0 + BN, sk + (buf ^ 1) * CHUNKS, sv + (buf ^ 1) * CHUNKS);
-        tile(std::false_type(), j0, buf);
-        if (more) stage.commit(sk + (buf ^ 1) * CHUNKS, sv + (buf ^ 1) * CHUNKS);
-    }
-    // A masked tile whose values are not all finite: 0 * NaN would carry them to rows that do not see
-    // them, so they count as zeros, and a second product counts those that a row sees.
+    auto arrive = [&]() INLINE { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
     __shared__ int s_bad[2];
-    for (; j0 < range.to; j0 += BN, buf ^= 1) {
-        if (tid == 0) s_bad[buf] = 0;
-        arrive();
-        const bool more = j0 + BN < range.to;
-        if (more) stage.fetch(j0 + BN, sk + (buf ^ 1) * CHUNKS, sv + (buf ^ 1) * CHUNKS);
-        uint32_t bad = 0;  // 8 bits for each of the thread's chunks
-        static_assert(CHUNKS == 4 * 64 * NW || CHUNKS == 2 * 64 * NW, "chunks of a thread");
+    // A masked tile whose values are not all finite: 0 * NaN would carry them to rows that do not see
+    // them.  A product of its own counts such values among those that a row sees, whose output
+    // becomes NaN, and they are zeros from then on.
+    auto check_values = [&](int j) INLINE {
+        u32x4 c[CHUNKS / (64 * NW)];
+        bool bad = false;
 #pragma unroll
         for (int i = 0; i < CHUNKS / (64 * NW); ++i) {
-            u32x4& c = sv[buf * CHUNKS + tid + i * 64 * NW];
-            const uint32_t b = nonfinite_bits(c);
-            if (b) c = clear_bits(c, b);
-            bad |= b << (8 * i);
+            c[i] = v_buf(b0)[tid + i * 64 * NW];
+            bad |= nonfinite_bits(c[i]) != 0;
         }
-        if (bad) s_bad[buf] = 1;
+        if (bad) s_bad[j & 1] = 1;
         lds_barrier();
-        if (j0 < wave_end) tile(std::true_type(), j0, buf);
-        if (s_bad[buf]) {
-            lds_barrier();
+        if (s_bad[j & 1] == 0) return;
 #pragma unroll
-            for (int i = 0; i < CHUNKS / (64 * NW); ++i) sv[buf * CHUNKS + tid + i * 64 * NW] = one_bits(bad >> (8 * i));
-            lds_barrier();
+        for (int i = 0; i < CHUNKS / (64 * NW); ++i) v_buf(b0)[tid + i * 64 * NW] = one_bits(nonfinite_bits(c[i]));
+        lds_barrier();
 #pragma unroll
-            for (int d = 0; d < ND; ++d) {
-                f32x16 count;
+        for (int d = 0; d < ND; ++d) {
+            f32x16 count;
 #pragma unroll
-                for (int i = 0; i < 16; ++i) count[i] = 0.f;
+            for (int i = 0; i < 16; ++i) count[i] = 0.f;
 #pragma unroll 1
-                for (int s = 0; s < 2 * NT; ++s) {
-                    bf16x8 seen;
+            for (int s = 0; s < 2 * NT; ++s) {
+                bf16x8 seen;
 #pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        seen[e] = (bf16)(j0 + 16 * s + 8 * (e >> 2) + 4 * h + (e & 3) <= my_pos ? 1.f : 0.f);
-                    count = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_frag(v_at + buf * CHUNKS * 16, d, s), seen, count, 0, 0, 0);
-                }
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (count[i] > 0.f) ot[d][i] = NAN;
+                for (int e = 0; e < 8; ++e)
+                    seen[e] = (bf16)(start(j) + 16 * s + 8 * (e >> 2) + 4 * h + (e & 3) <= my_pos ? 1.f : 0.f);
+                count = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_frag(v_at + b0, d, s), seen, count, 0, 0, 0);
             }
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (count[i] > 0.f) ot[d][i] = NAN;
         }
-        if (more) stage.commit(sk + (buf ^ 1) * CHUNKS, sv + (buf ^ 1) * CHUNKS);
+        lds_barrier();
+#pragma unroll
+        for (int i = 0; i < CHUNKS / (64 * NW); ++i) v_buf(b0)[tid + i * 64 * NW] = clear_bits(c[i], nonfinite_bits(c[i]));
+        lds_barrier();
+    };
+    // Two buffers, one barrier per tile.  Tiles that every row sees whole come first, without masks.
+    int j = 0;
+    for (; j < clear; ++j) {
+        arrive();
+        tile(false, j);
     }
-    const bool bad_page = stage.bad_page;
-    if (PAGED && __syncthreads_or(bad_page)) l = NAN;  // an invalid page was read
-    l += __shfl_xor(l, 32);
+    for (; j < tiles; ++j) {
+        if (tid == 0) s_bad[j & 1] = 0;
+        arrive();
+        check_values(j);
+        tile(true, j);
+    }
+    const bool lost = PAGED && __syncthreads_or(keys.bad_page || vals.bad_page);  // an invalid page was read
     if (row.kind == ROW_NONE) return;
+    const float sum = lost || row.kind == ROW_NAN ? NAN : row.kind == ROW_ZERO ? 0.f : half_sum(l);
     if (PAGED && p.splits > 1) {
         const int64_t at = (int64_t)split * p.n_tok * p.h_q + row.tok * p.h_q + row.head;
-        if (row.kind == ROW_NAN) l = NAN;
-        if (row.kind == ROW_ZERO) l = 0.f, m = -INFINITY;
         if (h == 0) {
-            p.part_ml[2 * at] = m;
-            p.part_ml[2 * at + 1] = l;
+            p.part_ml[2 * at] = row.kind == ROW_ZERO ? -INFINITY : m;
+            p.part_ml[2 * at + 1] = sum;
         }
-        if (l == 0.f) return;  // not read
+        if (sum == 0.f) return;  // not read
 #pragma unroll
         for (int t = 0; t < ND; ++t)
 #pragma unroll
@@ -405,16 +408,14 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_tile_kernel(AttnArgs p) {
                     f32x4{ot[t][4 * i], ot[t][4 * i + 1], ot[t][4 * i + 2], ot[t][4 * i + 3]};
         return;
     }
-    float inv = l == 0.f ? 0.f : 1.f / l;
-    if (row.kind == ROW_NAN) inv = NAN;
-    const bool zero = row.kind == ROW_ZERO || l == 0.f;
+    const float inv = 1.f / sum;
     bf16* o = reinterpret_cast<bf16*>(p.o) + (row.tok * p.h_q + row.head) * D;
 #pragma unroll
     for (int t = 0; t < ND; ++t)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const f32x4 y = f32x4{ot[t][4 * i], ot[t][4 * i + 1], ot[t][4 * i + 2], ot[t][4 * i + 3]} * inv;
-            *reinterpret_cast<bf16x4*>(o + 32 * t + 8 * i + 4 * h) = zero ? zero_bf16x4() : to_bf16(y);
+            *reinterpret_cast<bf16x4*>(o + 32 * t + 8 * i + 4 * h) = sum == 0.f ? zero_bf16x4() : to_bf16(y);
         }
 }
 
