@@ -120,6 +120,28 @@ __device__ __forceinline__ KeyRange key_range(int end, int splits, int s) {
     return KeyRange{(int)(a < end ? a : end), (int)(b < end ? b : end)};
 }
 
+// Eight bf16: bit i for an infinite or NaN element, the elements of set bits cleared, ones for set bits
+__device__ __forceinline__ uint32_t nonfinite_bits(u32x4 x) {
+    uint32_t b = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        b |= (x[i] & 0x7f80u) == 0x7f80u ? 1u << (2 * i) : 0u;
+        b |= (x[i] & 0x7f800000u) == 0x7f800000u ? 2u << (2 * i) : 0u;
+    }
+    return b;
+}
+__device__ __forceinline__ u32x4 clear_bits(u32x4 x, uint32_t b) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] &= ((b >> (2 * i)) & 1 ? 0u : 0xffffu) | ((b >> (2 * i)) & 2 ? 0u : 0xffff0000u);
+    return x;
+}
+__device__ __forceinline__ u32x4 one_bits(uint32_t b) {
+    u32x4 x;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = ((b >> (2 * i)) & 1 ? 0x3f80u : 0u) | ((b >> (2 * i)) & 2 ? 0x3f800000u : 0u);
+    return x;
+}
+
 // e4m3 pairs -> bf16 pairs times 2^e, exact; scale holds the power of two
 __device__ __forceinline__ uint32_t e4m3_pair(uint32_t x, float scale, bool hi) {
     const bf16x2 y = hi ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, scale, true)

@@ -55,6 +55,8 @@ constexpr int ATTN_ROWS_F32 = 64;
 
 hipError_t launch_attn(int d, int kind, bool paged, const AttnArgs& a, hipStream_t st);
 hipError_t launch_attn_f32(int d, bool paged, const AttnArgs& a, hipStream_t st);
+// few rows per request, in tiles of 16 or 32
+hipError_t launch_attn_few(int d, int kind, int rows, const AttnArgs& a, hipStream_t st);
 hipError_t launch_attn_join(int d, bool f32, const AttnArgs& a, hipStream_t st);
 hipError_t launch_kv_write(const KvArgs& a, hipStream_t st);
 hipError_t launch_kv_read(const KvArgs& a, hipStream_t st);

@@ -44,28 +44,6 @@ __device__ __forceinline__ int v_chunk(int r, int c) {
     return r * C + (c ^ f);
 }
 
-// Eight bf16: bit i for an infinite or NaN element, the elements of set bits cleared, ones for set bits
-__device__ __forceinline__ uint32_t nonfinite_bits(u32x4 x) {
-    uint32_t b = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        b |= (x[i] & 0x7f80u) == 0x7f80u ? 1u << (2 * i) : 0u;
-        b |= (x[i] & 0x7f800000u) == 0x7f800000u ? 2u << (2 * i) : 0u;
-    }
-    return b;
-}
-__device__ __forceinline__ u32x4 clear_bits(u32x4 x, uint32_t b) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] &= ((b >> (2 * i)) & 1 ? 0u : 0xffffu) | ((b >> (2 * i)) & 2 ? 0u : 0xffff0000u);
-    return x;
-}
-__device__ __forceinline__ u32x4 one_bits(uint32_t b) {
-    u32x4 x;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = ((b >> (2 * i)) & 1 ? 0x3f80u : 0u) | ((b >> (2 * i)) & 2 ? 0x3f800000u : 0u);
-    return x;
-}
-
 // Maximum and sum over the wave's two halves
 __device__ __forceinline__ float half_max(float x) {
     const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
@@ -321,13 +299,11 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_tile_kernel(AttnArgs p) {
                 }
                 pf[s] = __builtin_bit_cast(bf16x8, x);
             }
-            __builtin_amdgcn_s_setprio(1);
 #pragma unroll
             for (int s = 0; s < 2; ++s)
 #pragma unroll
                 for (int d = 0; d < ND; ++d)
                     ot[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_frag(v_at + b0, d, 2 * t + s), pf[s], ot[d], 0, 0, 0);
-            __builtin_amdgcn_s_setprio(0);
         }
         if (more) {
             keys.commit(k_buf(b1));

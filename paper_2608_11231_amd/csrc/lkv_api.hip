@@ -594,21 +594,36 @@ AttnArgs attn_args(const lkv_attn* A, const int32_t* cu, int32_t n_req, int64_t 
     a.h_kv = A->h_kv;
     a.group = A->h_q / A->h_kv;
     a.scale_log2 = A->scale * 1.4426950408889634f;
-    a.splits = 1;
-    const int rows = A->io_dtype == LKV_F32 ? ATTN_ROWS_F32 : ATTN_ROWS;
-    a.n_units = (int32_t)(n_req + (n_tok * a.group - 1) / rows);
     return a;
 }
 
-// Parts of the key range of a paged call: enough workgroups for the 256 CUs, none below 256 keys
-int attn_splits(const lkv_attn* A, int32_t n_req, int64_t n_tok, int32_t max_pages) {
-    const int rows = A->io_dtype == LKV_F32 ? ATTN_ROWS_F32 : ATTN_ROWS;
-    const int64_t wgs = (n_req + (n_tok * (A->h_q / A->h_kv) - 1) / rows) * (int64_t)A->h_kv;
-    if (wgs >= 512) return 1;
-    int64_t s = (1024 + wgs - 1) / wgs;
+// Row tiles and key parts of a call.  The number of (request, row tile) pairs is at most n_units.
+struct AttnPlan {
+    int rows;     // of a tile
+    bool few;     // attn_few_kernel
+    int n_units;
+    int splits;
+};
+AttnPlan attn_plan(const lkv_attn* A, int32_t n_req, int64_t n_tok, bool paged, int32_t max_pages) {
+    AttnPlan p = {};
+    const int64_t rows = n_tok * (A->h_q / A->h_kv);
+    p.rows = A->io_dtype == LKV_F32 ? ATTN_ROWS_F32 : ATTN_ROWS;
+    if (paged && A->io_dtype == LKV_BF16 && rows <= 32 * (int64_t)n_req) {
+        p.few = true;
+        p.rows = rows <= 16 * (int64_t)n_req ? 16 : 32;
+    }
+    p.n_units = (int)(n_req + (rows - 1) / p.rows);
+    p.splits = 1;
+    if (!paged) return p;
+    // enough workgroups for the CUs, none below 256 keys
+    const int64_t wgs = (int64_t)(p.few ? (rows + p.rows - 1) / p.rows : p.n_units) * A->h_kv;
+    const int64_t want = p.few ? 2048 : 512;
+    if (wgs >= want) return p;
+    int64_t s = ((p.few ? want : 1024) + wgs - 1) / wgs;
     const int64_t most = ((int64_t)max_pages * A->page + 255) / 256;
     s = s < most ? s : most;
-    return (int)(s < 1 ? 1 : (s > 128 ? 128 : s));
+    p.splits = (int)(s < 1 ? 1 : (s > 128 ? 128 : s));
+    return p;
 }
 
 struct AttnWs {
@@ -907,6 +922,8 @@ lkv_status lkv_attn_prefill(const lkv_attn* A, const int32_t* cu, int32_t n_seq,
     a.v = v;
     a.k_stride = k_stride;
     a.v_stride = v_stride;
+    a.n_units = attn_plan(A, n_seq, n_tok, false, 0).n_units;
+    a.splits = 1;
     hipStream_t st = (hipStream_t)stream;
     return hip_status(A->io_dtype == LKV_F32 ? launch_attn_f32(A->d, false, a, st) : launch_attn(A->d, KV_BF16, false, a, st));
 }
@@ -927,7 +944,7 @@ lkv_status lkv_attn_paged_workspace(const lkv_attn* A, int32_t n_req, int64_t n_
     if (s == LKV_OK) s = check_counts(A, n_req, n_tok);
     if (s != LKV_OK) return s;
     if (max_pages < 0 || max_pages > INT32_MAX / A->page) return LKV_E_SHAPE;
-    *bytes = n_req == 0 || n_tok == 0 ? 0 : attn_ws(A, n_tok, attn_splits(A, n_req, n_tok, max_pages)).total;
+    *bytes = n_req == 0 || n_tok == 0 ? 0 : attn_ws(A, n_tok, attn_plan(A, n_req, n_tok, true, max_pages).splits).total;
     return LKV_OK;
 }
 
@@ -945,7 +962,9 @@ lkv_status lkv_attn_paged(const lkv_attn* A, const lkv_pages* P, const int32_t* 
     AttnArgs a = attn_args(A, cu, n_req, n_tok, q, q_stride, o);
     a.pos = pos;
     a.pg = pages_args(A, P);
-    a.splits = attn_splits(A, n_req, n_tok, P->max_pages);
+    const AttnPlan plan = attn_plan(A, n_req, n_tok, true, P->max_pages);
+    a.n_units = plan.n_units;
+    a.splits = plan.splits;
     const AttnWs w = attn_ws(A, n_tok, a.splits);
     if (w.total > 0) {
         if (!ws) return LKV_E_NULL;
@@ -956,7 +975,9 @@ lkv_status lkv_attn_paged(const lkv_attn* A, const lkv_pages* P, const int32_t* 
     }
     hipStream_t st = (hipStream_t)stream;
     const bool f32 = A->io_dtype == LKV_F32;
-    s = hip_status(f32 ? launch_attn_f32(A->d, true, a, st) : launch_attn(A->d, kv_kind(A), true, a, st));
+    s = hip_status(f32        ? launch_attn_f32(A->d, true, a, st)
+                   : plan.few ? launch_attn_few(A->d, kv_kind(A), plan.rows, a, st)
+                              : launch_attn(A->d, kv_kind(A), true, a, st));
     if (s != LKV_OK || a.splits == 1) return s;
     return hip_status(launch_attn_join(A->d, f32, a, st));
 }
