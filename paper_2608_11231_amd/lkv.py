@@ -338,33 +338,50 @@ def make_attn(h_q: int, h_kv: int, d: int, scale: Optional[float] = None, page: 
     cache = dtype_code(io_dtype) if cache_dtype is None else (
         E4M3 if cache_dtype == torch.float8_e4m3fn else dtype_code(cache_dtype))
     a = Attn(h_q, h_kv, d, page, dtype_code(io_dtype), cache, d ** -0.5 if scale is None else scale)
-    a._io = io_dtype
+    a._io, a._d, a._hq, a._hkv = io_dtype, d, h_q, h_kv
     a._cache = {F32: torch.float32, BF16: torch.bfloat16, E4M3: torch.float8_e4m3fn}[cache]
     return a
 
 
-def _index(t: torch.Tensor, what: str, rows: int, dim: int = 1):
-    if t.dtype != torch.int32 or t.dim() != dim or t.shape[0] < rows:
-        raise ValueError(f"{what}: int32 of {dim} dimension(s) and at least {rows} rows expected")
-    _here(t, what)
-    return _ptr(t)
+# The smallest calls are bound by these checks too (a cache write of 64 tokens: 7 us, 3 of them here), so
+# they read each property of a tensor once.
+def _current() -> int:
+    return _raw_device() if _raw_device is not None else torch.cuda.current_device()
 
 
 def _here(t: torch.Tensor, what: str):
-    if t.get_device() != (_raw_device() if _raw_device is not None else torch.cuda.current_device()):
+    if t.get_device() != _current():
         raise ValueError(f"{what}: not on the current GPU")
+
+
+def _index(t: torch.Tensor, what: str, rows: int, dim: int = 1):
+    shape = t.shape
+    if len(shape) != dim or shape[0] < rows or t.dtype is not torch.int32:
+        raise ValueError(f"{what}: int32 of {dim} dimension(s) and at least {rows} rows expected")
+    if not t.is_contiguous():
+        raise ValueError("lkv tensors must be contiguous")
+    if t.get_device() != _current():
+        raise ValueError(f"{what}: not on the current GPU")
+    return t.data_ptr()
 
 
 def _rows(a: Attn, t: torch.Tensor, n_tok: int, heads: int, what: str):
     """Pointer and token stride of a [n_tok, heads, d] tensor whose tokens may lie apart."""
-    d = a.d
-    if t.dim() != 3 or t.shape[0] < n_tok or t.shape[1] != heads or t.shape[2] != d or t.dtype != a._io:
-        raise ValueError(f"{what}: {a._io} [{n_tok}, {heads}, {d}] expected, got {t.dtype} {tuple(t.shape)}")
-    s0, s1, s2 = t.stride()
-    if s2 != 1 or (heads > 1 and s1 != d):
+    shape, stride, d = t.shape, t.stride(), a._d
+    if len(shape) != 3 or shape[0] < n_tok or shape[1] != heads or shape[2] != d or t.dtype is not a._io:
+        raise ValueError(f"{what}: {a._io} [{n_tok}, {heads}, {d}] expected, got {t.dtype} {tuple(shape)}")
+    if stride[2] != 1 or (stride[1] != d and heads > 1):
         raise ValueError(f"{what}: a token's heads must be contiguous")
-    _here(t, what)
-    return t.data_ptr(), (s0 if t.shape[0] > 1 else heads * d)
+    if t.get_device() != _current():
+        raise ValueError(f"{what}: not on the current GPU")
+    return t.data_ptr(), (stride[0] if shape[0] > 1 else heads * d)
+
+
+def _dense(a: Attn, t: torch.Tensor, n_tok: int, heads: int, what: str):
+    p, stride = _rows(a, t, n_tok, heads, what)
+    if stride != heads * a._d:
+        raise ValueError(f"{what}: must be contiguous")
+    return p
 
 
 def make_pages(attn: Attn, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, length: torch.Tensor,
@@ -395,7 +412,7 @@ def make_pages(attn: Attn, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor
 
 
 def _paged(attn: Attn, pages: Pages, cu: torch.Tensor, n_tok: int, pos: Optional[torch.Tensor]):
-    n_req = int(cu.shape[0]) - 1
+    n_req = cu.shape[0] - 1
     own = pages._attn
     if own is not attn and (own.h_kv, own.page, own.d, own.cache_dtype) != (attn.h_kv, attn.page, attn.d, attn.cache_dtype):
         raise ValueError("pages: made for another layer geometry")
@@ -408,20 +425,19 @@ def attn_prefill(attn: Attn, cu: torch.Tensor, n_tok: int, q: torch.Tensor, k: t
                  o: torch.Tensor, stream=None) -> None:
     """Causal attention over the packed sequences ``cu``.  q, o [n_tok, h_q, d], k, v [n_tok, h_kv, d]; the
     tokens of q, k and v may lie apart (views of one projection's output), o is dense."""
-    qp, qs = _rows(attn, q, n_tok, attn.h_q, "q")
-    kp, ks = _rows(attn, k, n_tok, attn.h_kv, "k")
-    vp, vs = _rows(attn, v, n_tok, attn.h_kv, "v")
-    _rows(attn, o, n_tok, attn.h_q, "o")
-    _check(load().lkv_attn_prefill(attn, _index(cu, "cu", 1), int(cu.shape[0]) - 1, n_tok, qp, qs, kp, ks, vp, vs,
-                                   _ptr(o), _stream(stream)), "lkv_attn_prefill")
+    qp, qs = _rows(attn, q, n_tok, attn._hq, "q")
+    kp, ks = _rows(attn, k, n_tok, attn._hkv, "k")
+    vp, vs = _rows(attn, v, n_tok, attn._hkv, "v")
+    _check(load().lkv_attn_prefill(attn, _index(cu, "cu", 1), cu.shape[0] - 1, n_tok, qp, qs, kp, ks, vp, vs,
+                                   _dense(attn, o, n_tok, attn._hq, "o"), _stream(stream)), "lkv_attn_prefill")
 
 
 def kv_write(attn: Attn, pages: Pages, cu: torch.Tensor, n_tok: int, k: torch.Tensor, v: torch.Tensor,
              pos: Optional[torch.Tensor] = None, stream=None) -> None:
     """Write tokens' k and v [n_tok, h_kv, d] to positions ``pos`` (default: the last) of their requests' contexts."""
     cup, n_req, posp = _paged(attn, pages, cu, n_tok, pos)
-    kp, ks = _rows(attn, k, n_tok, attn.h_kv, "k")
-    vp, vs = _rows(attn, v, n_tok, attn.h_kv, "v")
+    kp, ks = _rows(attn, k, n_tok, attn._hkv, "k")
+    vp, vs = _rows(attn, v, n_tok, attn._hkv, "v")
     _check(load().lkv_kv_write(attn, pages, cup, n_req, n_tok, posp, kp, ks, vp, vs, _stream(stream)), "lkv_kv_write")
 
 
@@ -429,8 +445,8 @@ def kv_read(attn: Attn, pages: Pages, cu: torch.Tensor, n_tok: int, k: torch.Ten
             pos: Optional[torch.Tensor] = None, stream=None) -> None:
     """Read the rows at positions ``pos`` (default: the last) of the requests' contexts into k and v."""
     cup, n_req, posp = _paged(attn, pages, cu, n_tok, pos)
-    kp, ks = _rows(attn, k, n_tok, attn.h_kv, "k")
-    vp, vs = _rows(attn, v, n_tok, attn.h_kv, "v")
+    kp, ks = _rows(attn, k, n_tok, attn._hkv, "k")
+    vp, vs = _rows(attn, v, n_tok, attn._hkv, "v")
     _check(load().lkv_kv_read(attn, pages, cup, n_req, n_tok, posp, kp, ks, vp, vs, _stream(stream)), "lkv_kv_read")
 
 
@@ -447,11 +463,11 @@ def attn_paged(attn: Attn, pages: Pages, cu: torch.Tensor, n_tok: int, q: torch.
     """Attention of new tokens q [n_tok, h_q, d] over the paged cache, at positions ``pos`` (default: the
     last of each context); ``ws`` is a device workspace tensor (None or empty if it needs 0 bytes)."""
     cup, n_req, posp = _paged(attn, pages, cu, n_tok, pos)
-    qp, qs = _rows(attn, q, n_tok, attn.h_q, "q")
-    _rows(attn, o, n_tok, attn.h_q, "o")
+    qp, qs = _rows(attn, q, n_tok, attn._hq, "q")
+    op = _dense(attn, o, n_tok, attn._hq, "o")
     ws_bytes = 0
     if ws is not None:
         ws_bytes = ws.numel() * ws.element_size()
         _here(ws, "ws")
-    _check(load().lkv_attn_paged(attn, pages, cup, n_req, n_tok, posp, qp, qs, _ptr(o),
+    _check(load().lkv_attn_paged(attn, pages, cup, n_req, n_tok, posp, qp, qs, op,
                                  _ptr(ws) if ws_bytes else None, ws_bytes, _stream(stream)), "lkv_attn_paged")
