@@ -58,7 +58,7 @@ __device__ __forceinline__ AttnUnit attn_unit(const int32_t* cu, int n_req, int6
             const int l = __builtin_amdgcn_readfirstlane((int)__builtin_ctzll(after));
             w.r = r0 + l;
             w.n = __builtin_amdgcn_readlane(n, l);
-            w.t0 = clamp_tok(cu[w.r], 0, n_tok);
+            w.t0 = __builtin_amdgcn_readlane((int)t0, l);  // n_tok is below 2^31
             const int m = __builtin_amdgcn_readlane(more, l);
             const int before = __builtin_amdgcn_readlane(incl, l) - m;
             w.row0 = (int64_t)(m - 1 - (left - before)) * BM;

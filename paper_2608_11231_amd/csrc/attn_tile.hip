@@ -210,10 +210,17 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_tile_kernel(AttnArgs p) {
         vals.fetch(range.from, sv);
     }
 
+    // At d = 256 registers are short by a few fragments of Q: those are read from LDS each time.  (Spilled ones
+    // would be worse than their number: a load from scratch waits for the next tile's loads before it.)
+    constexpr int QL = D == 256 ? 3 : 0;
+    __shared__ u32x4 sq[QL > 0 ? NW * QL * 64 : 1];
+    const uint32_t q_at = lds_offset(sq) + 16 * (wave * QL * 64 + lane);
     bf16x8 qf[NS];
     const bf16* q = reinterpret_cast<const bf16*>(p.q) + row.tok * p.q_stride + (int64_t)row.head * D;
 #pragma unroll
     for (int s = 0; s < NS; ++s) qf[s] = row.kind == ROW_NONE ? bf16x8{} : *reinterpret_cast<const bf16x8*>(q + 16 * s + 8 * h);
+#pragma unroll
+    for (int s = 0; s < QL; ++s) sq[wave * QL * 64 + s * 64 + lane] = __builtin_bit_cast(u32x4, qf[s]);
     f32x16 ot[ND];
 #pragma unroll
     for (int t = 0; t < ND; ++t)
@@ -244,7 +251,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_tile_kernel(AttnArgs p) {
         const bool more = j + 1 < tiles;
         if (more) {
             keys.fetch(start(j + 1), k_buf(b1));
-            vals.fetch(start(j + 1), v_buf(b1));
+            if (KIND != KV_E4M3) vals.fetch(start(j + 1), v_buf(b1));
         }
         f32x16 st[NT];
         __builtin_amdgcn_s_setprio(1);
@@ -253,7 +260,11 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_tile_kernel(AttnArgs p) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) st[t][i] = 0.f;
 #pragma unroll
-            for (int s = 0; s < NS; ++s) st[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_frag(k_at + b0, t, s), qf[s], st[t], 0, 0, 0);
+            for (int s = 0; s < NS; ++s) {
+                // Q's fragments in LDS are the wave's own
+                const bf16x8 y = s < QL ? frag_read(q_at + 1024 * s) : qf[s];
+                st[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_frag(k_at + b0, t, s), y, st[t], 0, 0, 0);
+            }
         }
         __builtin_amdgcn_s_setprio(0);
         if (masked) {
@@ -281,6 +292,10 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_tile_kernel(AttnArgs p) {
 #pragma unroll
                 for (int e = 0; e < 16; ++e) ot[t][e] *= scale;
         }
+        if (more) {
+            keys.commit(k_buf(b1));
+            if (KIND == KV_E4M3) vals.fetch(start(j + 1), v_buf(b1));  // through the registers that the keys left
+        }
         const float m_use = m == -INFINITY ? 0.f : m;  // only scores of -inf so far
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
@@ -305,10 +320,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_tile_kernel(AttnArgs p) {
                 for (int d = 0; d < ND; ++d)
                     ot[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_frag(v_at + b0, d, 2 * t + s), pf[s], ot[d], 0, 0, 0);
         }
-        if (more) {
-            keys.commit(k_buf(b1));
-            vals.commit(v_buf(b1));
-        }
+        if (more) vals.commit(v_buf(b1));
         const int x = b0;
         b0 = b1, b1 = x;
     };

@@ -619,11 +619,12 @@ AttnPlan attn_plan(const lkv_attn* A, int32_t n_req, int64_t n_tok, bool paged, 
     // requests leave CUs idle, one round of the 512 workgroups that the GPU holds (four contexts of 8K,
     // 8 heads: 28.7 us with 16 parts, 31.9 with 33); else more and smaller workgroups, so that the
     // longest contexts do not end alone (128 of 1K-8K: 264 us whole, 250 in 2, 246 in 4, 274 in 8
-    // parts).  Many rows: enough workgroups for two per CU.
+    // parts).  Many rows: two workgroups per CU (two chunks
+    // of 512 tokens, 130 workgroups: 430 us in 4 parts, 448 in 8, whose results cost more to join).
     const int64_t units = p.few && rows < (int64_t)n_req * p.rows ? n_req : p.n_units, wgs = units * A->h_kv;
     int64_t s = 1;
     if (p.few) s = wgs <= 256 ? 512 / wgs : (4096 + wgs - 1) / wgs;
-    else if (wgs < 512) s = (1024 + wgs - 1) / wgs;
+    else if (wgs < 512) s = (512 + wgs - 1) / wgs;
     const int64_t most = ((int64_t)max_pages * A->page + 255) / 256;
     s = s < most ? s : most;
     p.splits = (int)(s < 1 ? 1 : (s > 128 ? 128 : s));
