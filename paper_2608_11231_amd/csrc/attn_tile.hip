@@ -84,15 +84,16 @@ struct Stage {
     const char* base;  // the pool; packed sequences: the next tile's first row
     int64_t stride;    // elements between rows, packed sequences
     int hk, end, tid, lane, wave;
-    int off[PER];       // bytes from the tile's (its page's) first row, full tiles
-    int ids, ids_next;  // lane i: page of keys 16 i .. of the next tile to fetch, and of the one behind it
-    u32x4 r[PER];       // e4m3 pieces on their way
-    float scale[PER];
+    int off[PER];  // bytes from the tile's (its page's) first row, full tiles
+    u32x4 r[PER];  // e4m3 pieces on their way, and their rows' scales: not touched before commit
+    uint8_t exps[PER];
+    uint32_t put;  // e4m3: byte offset of the thread's first chunk in a buffer
     bool bad_page = false;
 
     __device__ __forceinline__ Stage(const AttnArgs& p_, const AttnUnit& w_, int hk_, int end_, int tid_)
         : p(p_), w(w_), base(reinterpret_cast<const char*>(PAGED ? (V ? p_.pg.v : p_.pg.k) : (V ? p_.v : p_.k))),
           stride(V ? p_.v_stride : p_.k_stride), hk(hk_), end(end_), tid(tid_), lane(tid_ & 63), wave(__builtin_amdgcn_readfirstlane(tid_ >> 6)) {
+        put = 16 * (V ? v_chunk<D>(tid / U, 2 * (tid % U)) : k_chunk<D>(tid / U, 2 * (tid % U)));
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             const int x = tid + i * 64 * NW, row = x / U, c = x % U;
@@ -102,18 +103,11 @@ struct Stage {
         }
     }
     __device__ __forceinline__ int row(int i) const { return (tid + i * 64 * NW) / U; }
-    __device__ __forceinline__ int load_ids(int j0) const {
-        if (!PAGED) return 0;
-        const int j = min(j0 + 16 * (lane & (BN / 16 - 1)), end - 1);
-        return p.pg.table[(int64_t)w.r * p.pg.max_pages + (j >> p.pg.page_shift)];
-    }
     __device__ __forceinline__ void begin(int j0) {
         if (!PAGED) base += ((w.t0 + j0) * stride + (int64_t)hk * D) * 2;
-        ids = load_ids(j0);
-        ids_next = load_ids(j0 + BN);
     }
-    // starts the fetch of the tile at j0; tiles are fetched in order
-    __device__ __forceinline__ void fetch(int j0, u32x4* lds) {
+    // starts the fetch of the tile at j0; tiles are fetched in order.  ids: lane i has the page of keys 16 i ..
+    __device__ __forceinline__ void fetch(int j0, u32x4* lds, int ids) {
         const bool full = j0 + BN <= end;
         const int mask = (1 << p.pg.page_shift) - 1;
 #pragma unroll
@@ -136,7 +130,7 @@ struct Stage {
             }
             if constexpr (KIND == KV_E4M3) {
                 r[i] = *reinterpret_cast<const u32x4*>(b + (uint32_t)o);
-                scale[i] = exp_scale((V ? p.pg.v_exp : p.pg.k_exp)[first + (uint32_t)o / (16 * U)]);
+                exps[i] = (V ? p.pg.v_exp : p.pg.k_exp)[first + (uint32_t)o / (16 * U)];
             } else {
                 typedef __attribute__((address_space(1))) const void global_t;
                 typedef __attribute__((address_space(3))) void lds_t;
@@ -144,20 +138,20 @@ struct Stage {
             }
         }
         if (!PAGED) base += BN * stride * 2;
-        ids = ids_next;
-        ids_next = load_ids(j0 + 2 * BN);
     }
-    // e4m3: the fetched tile into LDS
-    __device__ __forceinline__ void commit(u32x4* lds) {
+    // e4m3: the fetched tile into the buffer at byte offset `lds`.  The thread's pieces are a multiple of 16
+    // rows apart, where the chunks' permutation repeats.
+    __device__ __forceinline__ void commit(uint32_t lds) {
         if constexpr (KIND == KV_E4M3) {
+            static_assert(PER == 1 || 64 * NW / U % 16 == 0, "rows of a thread's pieces");
 #pragma unroll
             for (int i = 0; i < PER; ++i) {
-                const int x = tid + i * 64 * NW, row = x / U, c = x % U;
+                const float scale = exp_scale(exps[i]);
 #pragma unroll
                 for (int e = 0; e < 2; ++e)
-                    lds[V ? v_chunk<D>(row, 2 * c + e) : k_chunk<D>(row, 2 * c + e)] =
-                        u32x4{e4m3_pair(r[i][2 * e], scale[i], false), e4m3_pair(r[i][2 * e], scale[i], true),
-                              e4m3_pair(r[i][2 * e + 1], scale[i], false), e4m3_pair(r[i][2 * e + 1], scale[i], true)};
+                    *(lds_u32x4*)(uintptr_t)(((lds + put) ^ (16 * e)) + i * (64 * NW / U) * 2 * D) =
+                        u32x4{e4m3_pair(r[i][2 * e], scale, false), e4m3_pair(r[i][2 * e], scale, true),
+                              e4m3_pair(r[i][2 * e + 1], scale, false), e4m3_pair(r[i][2 * e + 1], scale, true)};
             }
         }
     }
@@ -203,11 +197,19 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_tile_kernel(AttnArgs p) {
     int b0 = 0, b1 = CHUNKS * 16;  // buffers of the tile at hand and of the next one
     auto k_buf = [&](int o) INLINE { return reinterpret_cast<u32x4*>(reinterpret_cast<char*>(sk) + o); };
     auto v_buf = [&](int o) INLINE { return reinterpret_cast<u32x4*>(reinterpret_cast<char*>(sv) + o); };
+    auto load_ids = [&](int j0) INLINE {
+        if (!PAGED) return 0;
+        const int j = min(j0 + 16 * (lane & (BN / 16 - 1)), end - 1);
+        return p.pg.table[(int64_t)w.r * p.pg.max_pages + (j >> p.pg.page_shift)];
+    };
+    int ids = 0;  // pages of the next tile to fetch
     if (tiles > 0) {
+        ids = load_ids(range.from);
         keys.begin(range.from);
         vals.begin(range.from);
-        keys.fetch(range.from, sk);
-        vals.fetch(range.from, sv);
+        keys.fetch(range.from, sk, ids);
+        vals.fetch(range.from, sv, ids);
+        ids = load_ids(start(1));
     }
 
     // At d = 256 registers are short by a few fragments of Q: those are read from LDS each time.  (Spilled ones
@@ -228,8 +230,8 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_tile_kernel(AttnArgs p) {
         for (int i = 0; i < 16; ++i) ot[t][i] = 0.f;
     float m = -INFINITY, l = 0.f;  // reference of the exponents (base 2, see below) and this half's sum
     if (tiles > 0) {
-        keys.commit(sk);
-        vals.commit(sv);
+        keys.commit(lds_offset(sk));
+        vals.commit(lds_offset(sv));
     }
 
     // Byte offsets of the lane's fragments; the chunks' permutation is an exclusive or, so the others are
@@ -250,8 +252,11 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_tile_kernel(AttnArgs p) {
     auto tile = [&](bool masked, int j) INLINE {
         const bool more = j + 1 < tiles;
         if (more) {
-            keys.fetch(start(j + 1), k_buf(b1));
-            if (KIND != KV_E4M3) vals.fetch(start(j + 1), v_buf(b1));
+            keys.fetch(start(j + 1), k_buf(b1), ids);
+            if (KIND != KV_E4M3) {
+                vals.fetch(start(j + 1), v_buf(b1), ids);
+                ids = load_ids(start(j + 2));
+            }
         }
         f32x16 st[NT];
         __builtin_amdgcn_s_setprio(1);
@@ -293,8 +298,11 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_tile_kernel(AttnArgs p) {
                 for (int e = 0; e < 16; ++e) ot[t][e] *= scale;
         }
         if (more) {
-            keys.commit(k_buf(b1));
-            if (KIND == KV_E4M3) vals.fetch(start(j + 1), v_buf(b1));  // through the registers that the keys left
+            keys.commit(lds_offset(sk) + b1);
+            if (KIND == KV_E4M3) {  // through the registers that the keys left
+                vals.fetch(start(j + 1), v_buf(b1), ids);
+                ids = load_ids(start(j + 2));
+            }
         }
         const float m_use = m == -INFINITY ? 0.f : m;  // only scores of -inf so far
 #pragma unroll
@@ -320,7 +328,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_tile_kernel(AttnArgs p) {
                 for (int d = 0; d < ND; ++d)
                     ot[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_frag(v_at + b0, d, 2 * t + s), pf[s], ot[d], 0, 0, 0);
         }
-        if (more) vals.commit(v_buf(b1));
+        if (more) vals.commit(lds_offset(sv) + b1);
         const int x = b0;
         b0 = b1, b1 = x;
     };
@@ -331,21 +339,22 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_tile_kernel(AttnArgs p) {
     // them.  A product of its own counts such values among those that a row sees, whose output
     // becomes NaN, and they are zeros from then on.
     auto check_values = [&](int j) INLINE {
-        u32x4 c[CHUNKS / (64 * NW)];
         bool bad = false;
 #pragma unroll
-        for (int i = 0; i < CHUNKS / (64 * NW); ++i) {
-            c[i] = v_buf(b0)[tid + i * 64 * NW];
-            bad |= nonfinite_bits(c[i]) != 0;
-        }
+        for (int i = 0; i < CHUNKS / (64 * NW); ++i) bad |= nonfinite_bits(v_buf(b0)[tid + i * 64 * NW]) != 0;
         if (bad) s_bad[j & 1] = 1;
         lds_barrier();
         if (s_bad[j & 1] == 0) return;
-#pragma unroll
-        for (int i = 0; i < CHUNKS / (64 * NW); ++i) v_buf(b0)[tid + i * 64 * NW] = one_bits(nonfinite_bits(c[i]));
+        for (int x = tid; x < CHUNKS; x += 64 * NW) {
+            const u32x4 c = v_buf(b0)[x];
+            const uint32_t bits = nonfinite_bits(c);
+            v_buf(b0)[x] = clear_bits(c, bits);
+            v_buf(b1)[x] = one_bits(bits);  // free until the next tile is sent for
+        }
         lds_barrier();
 #pragma unroll
         for (int d = 0; d < ND; ++d) {
+            __builtin_amdgcn_sched_barrier(0);
             f32x16 count;
 #pragma unroll
             for (int i = 0; i < 16; ++i) count[i] = 0.f;
@@ -355,15 +364,12 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_tile_kernel(AttnArgs p) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
                     seen[e] = (bf16)(start(j) + 16 * s + 8 * (e >> 2) + 4 * h + (e & 3) <= my_pos ? 1.f : 0.f);
-                count = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_frag(v_at + b0, d, s), seen, count, 0, 0, 0);
+                count = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_frag(v_at + b1, d, s), seen, count, 0, 0, 0);
             }
 #pragma unroll
             for (int i = 0; i < 16; ++i)
                 if (count[i] > 0.f) ot[d][i] = NAN;
         }
-        lds_barrier();
-#pragma unroll
-        for (int i = 0; i < CHUNKS / (64 * NW); ++i) v_buf(b0)[tid + i * 64 * NW] = clear_bits(c[i], nonfinite_bits(c[i]));
         lds_barrier();
     };
     // Two buffers, one barrier per tile.  Tiles that every row sees whole come first, without masks.
