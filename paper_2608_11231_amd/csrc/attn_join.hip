@@ -1,0 +1,85 @@
+#include "attn_device.h"
+
+namespace lkv {
+
+// Join of the key ranges' results: with m = max m_s, o = sum 2^(m_s - m) o_s / sum 2^(m_s - m) l_s.
+// A workgroup joins one row: every wave forms all weights, a part per lane, and adds a quarter of
+// the parts, whose loads do not wait for each other; the quarters meet in LDS.  Short chains of
+// loads are what counts here: a decoding call waits for it.
+constexpr int JOIN_PARTS = 128;
+template <int D, typename T>
+__global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs p) {
+    constexpr int E = D / 64;  // elements of a lane
+    __shared__ float so[3][D];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t rows = p.n_tok * p.h_q, at = blockIdx.x;
+    const int64_t tok = at / p.h_q;
+    if (tok < clamp_tok(p.cu[0], 0, p.n_tok) || tok >= clamp_tok(p.cu[p.n_req], 0, p.n_tok)) return;
+    float ms[JOIN_PARTS / 64], ls[JOIN_PARTS / 64], m = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < JOIN_PARTS / 64; ++i) {
+        const int s = lane + 64 * i;
+        const bool in = s < p.splits;
+        ms[i] = in ? p.part_ml[2 * (s * rows + at)] : -INFINITY;
+        ls[i] = in ? p.part_ml[2 * (s * rows + at) + 1] : 0.f;
+        m = fmaxf(m, ms[i]);
+    }
+    for (int i = 1; i < 64; i <<= 1) m = fmaxf(m, __shfl_xor(m, i));
+    const float m_use = m == -INFINITY ? 0.f : m;
+    float f[JOIN_PARTS / 64], l = 0.f;
+#pragma unroll
+    for (int i = 0; i < JOIN_PARTS / 64; ++i) {
+        f[i] = ls[i] == 0.f ? 0.f : __builtin_amdgcn_exp2f(ms[i] - m_use);
+        l += f[i] * ls[i];
+    }
+    for (int i = 1; i < 64; i <<= 1) l += __shfl_xor(l, i);
+    float o[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] = 0.f;
+    const float* part = p.part_o + at * D + E * lane;
+#pragma unroll
+    for (int i = 0; i < JOIN_PARTS / 64; ++i) {
+        const int to = min(64 * (i + 1), p.splits);
+        for (int s0 = 64 * i + wave; s0 < to; s0 += 32) {
+            float y[8][E];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const int s = min(s0 + 4 * k, to - 1);
+#pragma unroll
+                for (int e = 0; e < E; ++e) y[k][e] = part[s * rows * D + e];
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const int s = s0 + 4 * k;
+                const float w = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, f[i]), s & 63));
+#pragma unroll
+                for (int e = 0; e < E; ++e) o[e] += s < to && w != 0.f ? w * y[k][e] : 0.f;  // parts without keys are not written
+            }
+        }
+    }
+    if (wave > 0)
+#pragma unroll
+        for (int e = 0; e < E; ++e) so[wave - 1][E * lane + e] = o[e];
+    __syncthreads();
+    if (wave > 0) return;
+    const float inv = 1.f / l;
+    T* out = reinterpret_cast<T*>(p.o) + at * D + E * lane;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        const int x = E * lane + e;
+        out[e] = (T)(l == 0.f ? 0.f : (o[e] + so[0][x] + so[1][x] + so[2][x]) * inv);
+    }
+}
+
+hipError_t launch_attn_join(int d, bool f32, const AttnArgs& a, hipStream_t st) {
+    const dim3 grid((unsigned)(a.n_tok * a.h_q)), block(256);
+    if (d == 64 && f32) hipLaunchKernelGGL((attn_join_kernel<64, float>), grid, block, 0, st, a);
+    else if (d == 64) hipLaunchKernelGGL((attn_join_kernel<64, bf16>), grid, block, 0, st, a);
+    else if (d == 128 && f32) hipLaunchKernelGGL((attn_join_kernel<128, float>), grid, block, 0, st, a);
+    else if (d == 128) hipLaunchKernelGGL((attn_join_kernel<128, bf16>), grid, block, 0, st, a);
+    else if (d == 256 && !f32) hipLaunchKernelGGL((attn_join_kernel<256, bf16>), grid, block, 0, st, a);
+    else return hipErrorInvalidValue;
+    return hipGetLastError();
+}
+
+}  // namespace lkv

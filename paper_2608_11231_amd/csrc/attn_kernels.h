@@ -51,7 +51,7 @@ struct KvArgs {
 
 // rows of one workgroup's tile
 constexpr int ATTN_ROWS = 128;
-constexpr int ATTN_ROWS_F32 = 64;
+constexpr int ATTN_ROWS_F32 = 32;
 
 hipError_t launch_attn(int d, int kind, bool paged, const AttnArgs& a, hipStream_t st);
 hipError_t launch_attn_f32(int d, bool paged, const AttnArgs& a, hipStream_t st);

@@ -402,14 +402,23 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_tile_kernel(AttnArgs p) {
                     f32x4{ot[t][4 * i], ot[t][4 * i + 1], ot[t][4 * i + 2], ot[t][4 * i + 3]};
         return;
     }
+    // Two groups of four of the lane's values, exchanged between the halves, make 16 adjacent bytes
     const float inv = 1.f / sum;
     bf16* o = reinterpret_cast<bf16*>(p.o) + (row.tok * p.h_q + row.head) * D;
 #pragma unroll
     for (int t = 0; t < ND; ++t)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const f32x4 y = f32x4{ot[t][4 * i], ot[t][4 * i + 1], ot[t][4 * i + 2], ot[t][4 * i + 3]} * inv;
-            *reinterpret_cast<bf16x4*>(o + 32 * t + 8 * i + 4 * h) = sum == 0.f ? zero_bf16x4() : to_bf16(y);
+        for (int i = 0; i < 4; i += 2) {
+            u32x4 y;
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int a = 4 * i + 2 * e, c = a + 4;
+                const auto r = __builtin_amdgcn_permlane32_swap(pack_bf16x2(ot[t][a] * inv, ot[t][a + 1] * inv),
+                                                                pack_bf16x2(ot[t][c] * inv, ot[t][c + 1] * inv), false, false);
+                y[e] = r[0], y[2 + e] = r[1];
+            }
+            if (sum == 0.f) y = u32x4{0, 0, 0, 0};
+            *reinterpret_cast<u32x4*>(o + 32 * t + 8 * i + 8 * h) = y;
         }
 }
 
