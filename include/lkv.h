@@ -405,10 +405,11 @@ typedef struct {
 /* Paged cache of one layer.
  *   k, v     [n_page, h_kv, page, d] cache_dtype, device
  *   k_exp, v_exp  LKV_E4M3: [n_page, h_kv, page] uint8, device: a row of codes c
- *            stands for c * 2^(exp - 127); otherwise NULL
+ *            stands for c * 2^(exp - 127), exp in [27, 247]; otherwise NULL
  *   table    device int32 [n_req, max_pages]: request r's token at position p is
  *            in slot p % page of page table[r][p / page].  Entries past the
- *            context are not read.  Requests may share pages.
+ *            context are not read.  Requests may share pages.  max_pages * page
+ *            is at most 2^30.
  *   len      device int32 [n_req]: tokens in each context, the new ones included
  *            (clamped to [0, max_pages * page], and to 0 if n_page is 0)
  * A page id outside [0, n_page) is never followed: a write to it is dropped, a

@@ -29,28 +29,31 @@ struct AttnUnit {
 // first, as unit u = request, found without looking at the other requests (decoding has only
 // these); then the other tiles request by request, from the last on, found by a scan over the
 // requests' tile counts.  The host knows only n_tok, so it launches n_req + (n_tok * group - 1) /
-// BM units, which bounds the number of tiles; the surplus leaves at once.
+// BM units, which bounds the number of tiles; the surplus leaves at once, and so do the units of
+// requests that another launch of the call takes.
 template <int BM>
-__device__ __forceinline__ AttnUnit attn_unit(const int32_t* cu, int n_req, int64_t n_tok, int group, int u, int lane) {
+__device__ __forceinline__ AttnUnit attn_unit(const AttnArgs& p, int u, int lane) {
     AttnUnit w{-1, 0, 0, 0};
-    auto tokens = [&](int r, int64_t& t0) {
-        t0 = clamp_tok(cu[r], 0, n_tok);
-        return (int)(clamp_tok(cu[r + 1], t0, n_tok) - t0);
+    auto tokens = [&](int r, int64_t& t0) {  // 0 for requests that are not the launch's
+        t0 = clamp_tok(p.cu[r], 0, p.n_tok);
+        const int n = (int)(clamp_tok(p.cu[r + 1], t0, p.n_tok) - t0);
+        const int64_t rows = (int64_t)n * p.group;
+        return rows >= p.rows_from && rows <= p.rows_to ? n : 0;
     };
-    if (u < n_req) {
+    if (u < p.n_req) {
         w.n = tokens(u, w.t0);
-        const int64_t rows = (int64_t)w.n * group;
+        const int64_t rows = (int64_t)w.n * p.group;
         if (rows == 0) return w;
         w.r = u;
         w.row0 = (rows - 1) / BM * BM;
         return w;
     }
-    int left = u - n_req;
-    for (int r0 = 0; r0 < n_req; r0 += 64) {
+    int left = u - p.n_req;
+    for (int r0 = 0; r0 < p.n_req; r0 += 64) {
         const int r = r0 + lane;
         int64_t t0 = 0;
-        const int n = r < n_req ? tokens(r, t0) : 0;
-        const int more = n > 0 ? (int)(((int64_t)n * group - 1) / BM) : 0;
+        const int n = r < p.n_req ? tokens(r, t0) : 0;
+        const int more = n > 0 ? (int)(((int64_t)n * p.group - 1) / BM) : 0;
         const int incl = wave_incl_scan_int(more);
         const int all = __builtin_amdgcn_readlane(incl, 63);
         if (left < all) {

@@ -29,7 +29,7 @@ __global__ __launch_bounds__(64 * NW) void attn_f32_kernel(AttnArgs p) {
     b /= p.h_kv;
     const int split = PAGED ? b % p.splits : 0;
     const int u = PAGED ? b / p.splits : b;
-    const AttnUnit w = attn_unit<BM>(p.cu, p.n_req, p.n_tok, p.group, u, lane);
+    const AttnUnit w = attn_unit<BM>(p, u, lane);
     if (w.r < 0) return;
     const int len = PAGED ? attn_len(p.pg, w.r) : w.n;
     const AttnRow row = attn_row<PAGED>(p, w, w.row0 + 16 * (wave & 1) + col, hk, len);

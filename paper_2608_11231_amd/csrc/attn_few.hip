@@ -49,7 +49,7 @@ __global__ __launch_bounds__(64 * NW, D * RT == 512 ? 1 : 2) void attn_few_kerne
     const int hk = b % p.h_kv;
     b /= p.h_kv;
     const int split = b % p.splits, u = b / p.splits;
-    const AttnUnit w = attn_unit<BM>(p.cu, p.n_req, p.n_tok, p.group, u, lane);
+    const AttnUnit w = attn_unit<BM>(p, u, lane);
     if (w.r < 0) return;
     const int len = attn_len(p.pg, w.r);
     AttnRow row[RT];

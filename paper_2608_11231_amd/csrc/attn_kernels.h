@@ -31,7 +31,8 @@ struct AttnArgs {
     int32_t h_q, h_kv, group;
     float scale_log2;  // softmax scale * log2(e)
     PagesArgs pg;
-    int32_t n_units;  // (request, row tile) slots, see attn_unit
+    int64_t rows_from, rows_to;  // the launch's requests: those of rows_from..rows_to rows (tokens * group)
+    int32_t n_units;             // (request, row tile) slots, see attn_unit
     int32_t splits;   // parts of the key range
     float* part_o;    // [splits, n_tok * h_q, d]
     float* part_ml;   // [splits, n_tok * h_q, 2]

@@ -523,6 +523,9 @@ lkv_status scratch_for_current_device(char** out) {
 
 // ---- full-attention layers
 
+// tokens of a context: positions a few tiles past the last one stay below 2^31
+constexpr int32_t MAX_CONTEXT = 1 << 30;
+
 lkv_status check_attn(const lkv_attn* A) {
     if (!A) return LKV_E_NULL;
     if (A->h_q < 1 || A->h_kv < 1 || A->h_q % A->h_kv != 0 || A->d < 1 || A->page < 1) return LKV_E_SHAPE;
@@ -557,7 +560,7 @@ lkv_status check_rows(const lkv_attn* A, const void* x, int64_t stride, int32_t 
 
 lkv_status check_pages(const lkv_attn* A, const lkv_pages* P) {
     if (!P) return LKV_E_NULL;
-    if (P->n_page < 0 || P->max_pages < 0 || P->max_pages > INT32_MAX / A->page) return LKV_E_SHAPE;
+    if (P->n_page < 0 || P->max_pages < 0 || P->max_pages > MAX_CONTEXT / A->page) return LKV_E_SHAPE;
     if (!P->len || (P->max_pages > 0 && !P->table)) return LKV_E_NULL;
     if (P->n_page > 0) {
         if (!P->k || !P->v) return LKV_E_NULL;
@@ -593,38 +596,55 @@ AttnArgs attn_args(const lkv_attn* A, const int32_t* cu, int32_t n_req, int64_t 
     a.h_q = A->h_q;
     a.h_kv = A->h_kv;
     a.group = A->h_q / A->h_kv;
+    a.rows_to = INT64_MAX;
     a.scale_log2 = A->scale * 1.4426950408889634f;
     return a;
 }
 
-// Row tiles and key parts of a call.  The number of (request, row tile) pairs is at most n_units.
+// Launches of a call: its requests of few rows and the others each have a kernel, where the requests
+// can be of either kind.  The lengths are on the device, so the host goes by their mean: up to 32 rows
+// the few-row kernel takes all (a longer request among them just has more tiles), above it each
+// takes its own (100 decoding requests beside a chunk of 512 tokens), of one request only the tiles.
 struct AttnPlan {
-    int rows;     // of a tile
-    bool few;     // attn_few_kernel
-    int n_units;
+    int few_rows;   // row tile of attn_few_kernel, 0: not launched
+    int few_units;  // (request, row tile) pairs at most
+    int tile_units;  // of the tile kernels, 0: not launched
     int splits;
 };
+constexpr int FEW_ROWS = 32;
 AttnPlan attn_plan(const lkv_attn* A, int32_t n_req, int64_t n_tok, bool paged, int32_t max_pages) {
     AttnPlan p = {};
     const int64_t rows = n_tok * (A->h_q / A->h_kv);
-    p.rows = A->io_dtype == LKV_F32 ? ATTN_ROWS_F32 : ATTN_ROWS;
-    if (paged && A->io_dtype == LKV_BF16 && rows <= 32 * (int64_t)n_req) {
-        p.few = true;
-        p.rows = rows <= 16 * (int64_t)n_req ? 16 : 32;
-    }
-    p.n_units = (int)(n_req + (rows - 1) / p.rows);
+    const int tile = A->io_dtype == LKV_F32 ? ATTN_ROWS_F32 : ATTN_ROWS;
+    auto units = [&](int tile_rows) { return (int)(n_req + (rows - 1) / tile_rows); };
     p.splits = 1;
-    if (!paged) return p;
+    if (!paged || A->io_dtype == LKV_F32) {
+        p.tile_units = units(tile);
+        if (!paged) return p;
+    } else if (rows <= FEW_ROWS * (int64_t)n_req) {
+        p.few_rows = rows <= 16 * (int64_t)n_req ? 16 : 32;
+        p.few_units = units(p.few_rows);
+    } else {
+        p.tile_units = units(tile);
+        if (n_req > 1) {
+            p.few_rows = 32;
+            p.few_units = n_req;  // one tile each
+        }
+    }
     // Parts of the key range, none below 256 keys of the longest context.  Few rows: where the
     // requests leave CUs idle, one round of the 512 workgroups that the GPU holds (four contexts of 8K,
     // 8 heads: 28.7 us with 16 parts, 31.9 with 33); else more and smaller workgroups, so that the
     // longest contexts do not end alone (128 of 1K-8K: 264 us whole, 250 in 2, 246 in 4, 274 in 8
     // parts).  Many rows: two workgroups per CU (two chunks
     // of 512 tokens, 130 workgroups: 430 us in 4 parts, 448 in 8, whose results cost more to join).
-    const int64_t units = p.few && rows < (int64_t)n_req * p.rows ? n_req : p.n_units, wgs = units * A->h_kv;
     int64_t s = 1;
-    if (p.few) s = wgs <= 256 ? 512 / wgs : (4096 + wgs - 1) / wgs;
-    else if (wgs < 512) s = (512 + wgs - 1) / wgs;
+    if (p.tile_units == 0) {
+        const int64_t wgs = (rows < (int64_t)n_req * p.few_rows ? n_req : p.few_units) * (int64_t)A->h_kv;
+        s = wgs <= 256 ? 512 / wgs : (4096 + wgs - 1) / wgs;
+    } else {
+        const int64_t wgs = (int64_t)p.tile_units * A->h_kv;
+        if (wgs < 512) s = (512 + wgs - 1) / wgs;
+    }
     const int64_t most = ((int64_t)max_pages * A->page + 255) / 256;
     s = s < most ? s : most;
     p.splits = (int)(s < 1 ? 1 : (s > 128 ? 128 : s));
@@ -927,7 +947,7 @@ lkv_status lkv_attn_prefill(const lkv_attn* A, const int32_t* cu, int32_t n_seq,
     a.v = v;
     a.k_stride = k_stride;
     a.v_stride = v_stride;
-    a.n_units = attn_plan(A, n_seq, n_tok, false, 0).n_units;
+    a.n_units = attn_plan(A, n_seq, n_tok, false, 0).tile_units;
     a.splits = 1;
     hipStream_t st = (hipStream_t)stream;
     return hip_status(A->io_dtype == LKV_F32 ? launch_attn_f32(A->d, false, a, st) : launch_attn(A->d, KV_BF16, false, a, st));
@@ -948,7 +968,7 @@ lkv_status lkv_attn_paged_workspace(const lkv_attn* A, int32_t n_req, int64_t n_
     lkv_status s = check_attn(A);
     if (s == LKV_OK) s = check_counts(A, n_req, n_tok);
     if (s != LKV_OK) return s;
-    if (max_pages < 0 || max_pages > INT32_MAX / A->page) return LKV_E_SHAPE;
+    if (max_pages < 0 || max_pages > MAX_CONTEXT / A->page) return LKV_E_SHAPE;
     *bytes = n_req == 0 || n_tok == 0 ? 0 : attn_ws(A, n_tok, attn_plan(A, n_req, n_tok, true, max_pages).splits).total;
     return LKV_OK;
 }
@@ -968,7 +988,6 @@ lkv_status lkv_attn_paged(const lkv_attn* A, const lkv_pages* P, const int32_t* 
     a.pos = pos;
     a.pg = pages_args(A, P);
     const AttnPlan plan = attn_plan(A, n_req, n_tok, true, P->max_pages);
-    a.n_units = plan.n_units;
     a.splits = plan.splits;
     const AttnWs w = attn_ws(A, n_tok, a.splits);
     if (w.total > 0) {
@@ -980,9 +999,18 @@ lkv_status lkv_attn_paged(const lkv_attn* A, const lkv_pages* P, const int32_t* 
     }
     hipStream_t st = (hipStream_t)stream;
     const bool f32 = A->io_dtype == LKV_F32;
-    s = hip_status(f32        ? launch_attn_f32(A->d, true, a, st)
-                   : plan.few ? launch_attn_few(A->d, kv_kind(A), plan.rows, a, st)
-                              : launch_attn(A->d, kv_kind(A), true, a, st));
+    if (plan.tile_units > 0) {
+        a.n_units = plan.tile_units;
+        a.rows_from = plan.few_rows > 0 ? FEW_ROWS + 1 : 0;
+        s = hip_status(f32 ? launch_attn_f32(A->d, true, a, st) : launch_attn(A->d, kv_kind(A), true, a, st));
+        if (s != LKV_OK) return s;
+    }
+    if (plan.few_rows > 0) {
+        a.n_units = plan.few_units;
+        a.rows_from = 0;
+        if (plan.tile_units > 0) a.rows_to = FEW_ROWS;
+        s = hip_status(launch_attn_few(A->d, kv_kind(A), plan.few_rows, a, st));
+    }
     if (s != LKV_OK || a.splits == 1) return s;
     return hip_status(launch_attn_join(A->d, f32, a, st));
 }

@@ -407,7 +407,7 @@ def make_pages(attn: Attn, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor
     p.len = _index(length, "length", table.shape[0])
     p.n_page, p.max_pages = int(k.shape[0]), int(table.shape[1])
     p._keep = (k, v, table, length, k_exp, v_exp)
-    p._n_req, p._attn = int(table.shape[0]), attn
+    p._n_req, p._attn, p._dev = int(table.shape[0]), attn, k.get_device()
     return p
 
 
@@ -416,6 +416,8 @@ def _paged(attn: Attn, pages: Pages, cu: torch.Tensor, n_tok: int, pos: Optional
     own = pages._attn
     if own is not attn and (own.h_kv, own.page, own.d, own.cache_dtype) != (attn.h_kv, attn.page, attn.d, attn.cache_dtype):
         raise ValueError("pages: made for another layer geometry")
+    if pages._dev != _current():
+        raise ValueError("pages: not on the current GPU")
     if n_req > pages._n_req:
         raise ValueError("pages: fewer rows in the table than requests")
     return _index(cu, "cu", 1), n_req, None if pos is None else _index(pos, "pos", n_tok)

@@ -348,6 +348,53 @@ def test_paged_values_not_seen(cache):
     assert torch.equal(bad[:3], good[:3]) and bool(bad[3:].isnan().all())
 
 
+@pytest.mark.parametrize("hq,hkv,d,cache", [(8, 2, 128, BF), (8, 1, 64, E4), (16, 2, 256, E4)])
+def test_paged_mixed_batch(hq, hkv, d, cache):
+    """Decoding requests beside chunks, empty requests among them: every request is taken once."""
+    attn = lkv.make_attn(hq, hkv, d, page=16, cache_dtype=cache)
+    new = [1, 130, 0, 1, 4, 8, 9, 33, 1, 0, 2]
+    ctx = [40, 300, 10, 1, 4, 700, 90, 33, 2000, 0, 64]
+    C = Cache(attn, ctx)
+    C.fill()
+    q = _qkv(sum(new) + 1, hq, 1, d, BF, 6)[0]
+    _check_paged(attn, C, new, q, _attn_paged(attn, C, _cum(new), q))
+
+
+def test_far_offsets():
+    """Rows and pages whose byte offsets pass 32 bits."""
+    n, far = 530, 1 << 22  # 530 rows 2^22 elements apart: 4.4 GB
+    x = torch.empty(n * far, dtype=BF, device="cuda")
+    small = _qkv(n, 2, 1, 64, BF, 3, False)
+    views, at = [], 0
+    for t in small:
+        y = x.as_strided((n, t.shape[1], 64), (far, 64, 1), at)
+        y.copy_(t)
+        views.append(y)
+        at += t.shape[1] * 64
+    attn = lkv.make_attn(2, 1, 64, page=16)
+    o, o2 = torch.empty_like(small[0]), torch.empty_like(small[0])
+    cu = _i32([0, 200, n])
+    lkv.attn_prefill(attn, cu, n, *small, o)
+    lkv.attn_prefill(attn, cu, n, *views, o2)
+    assert torch.equal(o, o2)
+    del x, views, y
+    pool = (1 << 32) // (16 * 64) // 2 + 200  # pages of 2 KB: past 4 GB
+    k, v = (torch.empty((pool, 1, 16, 64), dtype=BF, device="cuda") for _ in range(2))
+    ids = np.arange(pool - 40, pool, dtype=np.int32).reshape(1, 40)
+    P = lkv.make_pages(attn, k, v, _i32(ids), _i32([n]))
+    lkv.kv_write(attn, P, _i32([0, n]), n, small[1], small[2])
+    back = [torch.empty_like(t) for t in small[1:]]
+    lkv.kv_read(attn, P, _i32([0, n]), n, *back)
+    torch.cuda.synchronize()
+    assert torch.equal(back[0], small[1]) and torch.equal(back[1], small[2])
+    for m in (1, 60):
+        q = small[0][:m].contiguous()
+        ws = torch.empty(lkv.attn_paged_workspace(attn, 1, m, 40), dtype=torch.uint8, device="cuda")
+        om = torch.empty_like(q)
+        lkv.attn_paged(attn, P, _i32([0, m]), m, q, om, ws)
+        _close(om, A.attention(_np(q), _np(small[1]), _np(small[2]), np.arange(n - m, n), attn.scale))
+
+
 # ---------------------------------------------------------------- together
 @pytest.mark.parametrize("cache", [BF, E4], ids=["bf16", "e4m3"])
 def test_reuse_flow(cache):
