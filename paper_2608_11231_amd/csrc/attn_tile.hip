@@ -175,12 +175,17 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_tile_kernel(AttnArgs p) {
     const AttnUnit w = attn_unit<BM>(p, u, lane);
     if (w.r < 0) return;
     const int len = PAGED ? attn_len(p.pg, w.r) : w.n;
-    const AttnRow row = attn_row<PAGED>(p, w, w.row0 + 32 * wave + col, hk, len);
-    const bool sees = row.kind == ROW_SEES;
-    const int my_pos = sees ? row.pos : 0x7fffffff;
+    // The lane's row; at d = 256, short of registers, formed again after the unmasked tiles, not held over them
+    auto my_row = [&]() INLINE {
+        int c = col;
+        if (D == 256) asm volatile("" : "+v"(c));
+        return attn_row<PAGED>(p, w, w.row0 + 32 * wave + c, hk, len);
+    };
+    const AttnRow first_row = my_row();
+    const bool sees = first_row.kind == ROW_SEES;
     // keys that some row of the workgroup sees, and that all of its rows see
     __shared__ int s_end[NW], s_all[NW];
-    int end = wave_max_int(sees ? row.pos + 1 : 0), all = wave_min_int(sees ? row.pos + 1 : 0x7fffffff);
+    int end = wave_max_int(sees ? first_row.pos + 1 : 0), all = wave_min_int(sees ? first_row.pos + 1 : 0x7fffffff);
     if (lane == 0) s_end[wave] = end, s_all[wave] = all;
     __syncthreads();
 #pragma unroll
@@ -218,9 +223,9 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_tile_kernel(AttnArgs p) {
     __shared__ u32x4 sq[QL > 0 ? NW * QL * 64 : 1];
     const uint32_t q_at = lds_offset(sq) + 16 * (wave * QL * 64 + lane);
     bf16x8 qf[NS];
-    const bf16* q = reinterpret_cast<const bf16*>(p.q) + row.tok * p.q_stride + (int64_t)row.head * D;
+    const bf16* q = reinterpret_cast<const bf16*>(p.q) + first_row.tok * p.q_stride + (int64_t)first_row.head * D;
 #pragma unroll
-    for (int s = 0; s < NS; ++s) qf[s] = row.kind == ROW_NONE ? bf16x8{} : *reinterpret_cast<const bf16x8*>(q + 16 * s + 8 * h);
+    for (int s = 0; s < NS; ++s) qf[s] = first_row.kind == ROW_NONE ? bf16x8{} : *reinterpret_cast<const bf16x8*>(q + 16 * s + 8 * h);
 #pragma unroll
     for (int s = 0; s < QL; ++s) sq[wave * QL * 64 + s * 64 + lane] = __builtin_bit_cast(u32x4, qf[s]);
     f32x16 ot[ND];
@@ -248,6 +253,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_tile_kernel(AttnArgs p) {
         return __builtin_shufflevector(a, c, 0, 1, 2, 3, 4, 5, 6, 7);
     };
 
+    int my_pos = 0;  // set for the masked tiles
     // Tile j, whose keys and values are in the buffers at b0; the next one's are sent for.
     auto tile = [&](bool masked, int j) INLINE {
         const bool more = j + 1 < tiles;
@@ -378,6 +384,8 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_tile_kernel(AttnArgs p) {
         arrive();
         tile(false, j);
     }
+    const AttnRow row = my_row();
+    my_pos = row.kind == ROW_SEES ? row.pos : 0x7fffffff;
     for (; j < tiles; ++j) {
         if (tid == 0) s_bad[j & 1] = 0;
         arrive();
