@@ -1,8 +1,10 @@
 // Write and read of the paged key/value cache.
 //
-// One wave moves one token's k and v rows, in chunks of 16 elements per lane (16 bytes of e4m3).
-// The rows are read once and written once; both are bound by HBM for many tokens and by latency
-// for few, so the wave finds its request with one pass of ballots over the offsets.
+// A wave moves one token, its k and v rows in chunks of 16 elements per lane (16 bytes of e4m3).
+// Small calls are latency: the token's slot is a chain of loads (offsets, position and length,
+// page), which starts after the rows to write have been sent for.  Large ones are HBM traffic, each
+// row read once and written once: 32768 tokens of 8 heads of 128 in bf16, written and read back,
+// 110 us (4.9 TB/s; with four tokens a wave 119).
 //
 // e4m3 rows carry one power-of-two scale per (token, head).  A power of two costs a
 // floating-point code no precision, the scaling is exact, and so is the value read back: 4
@@ -13,52 +15,47 @@ namespace lkv {
 
 namespace {
 
-struct KvSlot {
-    int r;           // -1: token outside every request
-    int64_t row;     // pool row of head 0: (page * h_kv << shift) + slot; -1: no such position or page
-    bool duplicate;  // the next token of the request has the same position
-};
-
-// The request of token j is r with cu[r] <= j < cu[r + 1]; offsets are clamped to [0, n_tok].
-__device__ __forceinline__ KvSlot kv_slot(const KvArgs& p, int64_t j, int lane) {
-    KvSlot s{-1, -1, false};
-    int count = 0;  // offsets <= j
+// Where a token's rows are: pool row of head 0, (page * h_kv << shift) + slot
+constexpr int64_t NO_PLACE = -1;    // a position or page that does not exist
+constexpr int64_t NO_REQUEST = -2;  // a token outside every request, or (write) one that a later token replaces
+// The request of token j is r with cu[r] <= j < cu[r + 1], offsets clamped to [0, n_tok]: r + 1 is the
+// number of offsets <= j.
+template <bool WRITE>
+__device__ __forceinline__ int64_t kv_row(const KvArgs& p, int64_t j, int lane) {
+    int count = 0;
     for (int r0 = 0; r0 <= p.n_req; r0 += 64) {
-        const int r = r0 + lane;
-        const bool before = r <= p.n_req && clamp_tok(p.cu[r], 0, p.n_tok) <= j;
+        const bool before = r0 + lane <= p.n_req && clamp_tok(p.cu[r0 + lane], 0, p.n_tok) <= j;
         count += __builtin_popcountll(__ballot(before));
     }
     const int r = count - 1;
-    if (r < 0 || r >= p.n_req) return s;
+    if (r < 0 || r >= p.n_req) return NO_REQUEST;
     const int64_t t0 = clamp_tok(p.cu[r], 0, p.n_tok), t1 = clamp_tok(p.cu[r + 1], t0, p.n_tok);
-    if (j < t0 || j >= t1) return s;
-    s.r = r;
     const int len = attn_len(p.pg, r);
+    if (j < t0 || j >= t1) return NO_REQUEST;
     const int64_t pos = p.pos ? p.pos[j] : len - (t1 - j);
-    s.duplicate = p.pos && j + 1 < t1 && p.pos[j + 1] == pos;
-    if (pos < 0 || pos >= len) return s;
+    if (WRITE && p.pos && j + 1 < t1 && p.pos[j + 1] == pos) return NO_REQUEST;  // of such neighbours the last is written
+    if (pos < 0 || pos >= len) return NO_PLACE;
     const int page = p.pg.table[(int64_t)r * p.pg.max_pages + (pos >> p.pg.page_shift)];
-    if (page < 0 || page >= p.pg.n_page) return s;
-    s.row = (((int64_t)page * p.h_kv) << p.pg.page_shift) + (pos & ((1 << p.pg.page_shift) - 1));
-    return s;
+    if (page < 0 || page >= p.pg.n_page) return NO_PLACE;
+    return (((int64_t)page * p.h_kv) << p.pg.page_shift) + (pos & ((1 << p.pg.page_shift) - 1));
 }
 
-// 16 bf16 elements, widened
-struct Vals {
-    float x[16];
+// 16 elements as they lie in memory
+template <typename T>
+struct Raw {
+    u32x4 x[sizeof(T)];
 };
-__device__ __forceinline__ Vals load16(const bf16* s) {
-    Vals v;
+template <typename T>
+__device__ __forceinline__ Raw<T> load_raw(const void* s) {
+    Raw<T> r;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const u32x4 b = reinterpret_cast<const u32x4*>(s)[i];
+    for (int i = 0; i < (int)sizeof(T); ++i) r.x[i] = reinterpret_cast<const u32x4*>(s)[i];
+    return r;
+}
+template <typename T>
+__device__ __forceinline__ void store_raw(void* d, const Raw<T>& r) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            v.x[8 * i + 2 * e] = __builtin_bit_cast(float, b[e] << 16);
-            v.x[8 * i + 2 * e + 1] = __builtin_bit_cast(float, b[e] & 0xffff0000u);
-        }
-    }
-    return v;
+    for (int i = 0; i < (int)sizeof(T); ++i) reinterpret_cast<u32x4*>(d)[i] = r.x[i];
 }
 
 // Scale byte of a row whose largest finite magnitude is amax: 127 + the least e in [-100, 120]
@@ -69,106 +66,134 @@ __device__ __forceinline__ uint32_t scale_byte(float amax) {
     return (uint32_t)(127 + min(max(e, -100), 120));
 }
 
-template <typename T, bool E4M3>
-__device__ __forceinline__ void write_row(const KvArgs& p, const T* src, void* pages, uint8_t* exps, int64_t row, int lane,
-                                          bool active, int per_head, int c) {
-    // lanes of one head are adjacent, per_head of them (a power of two)
-    if constexpr (!E4M3) {
-        if (!active) return;
-        const u32x4* s = reinterpret_cast<const u32x4*>(src);
-        u32x4* d = reinterpret_cast<u32x4*>(reinterpret_cast<T*>(pages) + row * p.d + 16 * c);
+// Maximum over groups of 4, 8 or 16 adjacent lanes, in registers: neighbours, pairs, then mirrored halves
+__device__ __forceinline__ float group_max(float x, int lanes) {
+    x = fmaxf(x, dpp_mov<0xb1, 0xf, false>(x));   // quad_perm 1 0 3 2
+    x = fmaxf(x, dpp_mov<0x4e, 0xf, false>(x));   // quad_perm 2 3 0 1
+    if (lanes >= 8) x = fmaxf(x, dpp_mov<0x141, 0xf, false>(x));   // row_half_mirror
+    if (lanes >= 16) x = fmaxf(x, dpp_mov<0x140, 0xf, false>(x));  // row_mirror
+    return x;
+}
+
+// Codes of 16 bf16 and the scale byte of their row, which the per_head lanes of a head (adjacent, a power
+// of two) hold between them
+__device__ __forceinline__ u32x4 encode(const Raw<bf16>& r, int per_head, uint32_t& byte) {
+    float x[16], amax = 0.f;
 #pragma unroll
-        for (int i = 0; i < (int)sizeof(T); ++i) d[i] = s[i];
-        return;
-    } else {
-    Vals v = {};
-    if (active) v = load16(src);
-    float amax = 0.f;
+    for (int i = 0; i < 8; ++i) {
+        const uint32_t b = r.x[i / 4][i % 4];
+        x[2 * i] = __builtin_bit_cast(float, b << 16);
+        x[2 * i + 1] = __builtin_bit_cast(float, b & 0xffff0000u);
+    }
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-        const float a = __builtin_fabsf(v.x[i]);
+        const float a = __builtin_fabsf(x[i]);
         amax = a < INFINITY ? fmaxf(amax, a) : amax;  // infinities and NaN do not count and become NaN
     }
-    for (int i = 1; i < per_head; i <<= 1) amax = fmaxf(amax, __shfl_xor(amax, i));
-    const uint32_t byte = scale_byte(amax);
+    amax = group_max(amax, per_head);
+    byte = scale_byte(amax);
     const float inv = exp_scale((uint8_t)(254 - byte));  // 2^-e, exact
     u32x4 out;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         float y[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const float x = v.x[4 * i + e];
-            y[e] = __builtin_fabsf(x) < INFINITY ? x * inv : NAN;
-        }
+        for (int e = 0; e < 4; ++e) y[e] = __builtin_fabsf(x[4 * i + e]) < INFINITY ? x[4 * i + e] * inv : NAN;
         int word = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
         word = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], word, true);
         out[i] = (uint32_t)word;
     }
-    if (!active) return;
-    *reinterpret_cast<u32x4*>(reinterpret_cast<uint8_t*>(pages) + row * p.d + 16 * c) = out;
-    if (c == 0) exps[row] = (uint8_t)byte;
-    }
+    return out;
 }
-
-template <typename T, bool E4M3>
-__device__ __forceinline__ void read_row(const KvArgs& p, T* dst, const void* pages, const uint8_t* exps, int64_t row, int c) {
-    u32x4* d = reinterpret_cast<u32x4*>(dst);
-    if (row < 0) {
-        const uint32_t nan = sizeof(T) == 2 ? 0x7fc07fc0u : 0x7fc00000u;
+__device__ __forceinline__ Raw<bf16> decode(u32x4 b, uint8_t byte) {
+    const float s = exp_scale(byte);
+    Raw<bf16> r;
 #pragma unroll
-        for (int i = 0; i < (int)sizeof(T); ++i) d[i] = u32x4{nan, nan, nan, nan};
-    } else if constexpr (!E4M3) {
-        const u32x4* s = reinterpret_cast<const u32x4*>(reinterpret_cast<const T*>(pages) + row * p.d + 16 * c);
-#pragma unroll
-        for (int i = 0; i < (int)sizeof(T); ++i) d[i] = s[i];
-    } else {
-        const u32x4 b = *reinterpret_cast<const u32x4*>(reinterpret_cast<const uint8_t*>(pages) + row * p.d + 16 * c);
-        const float s = exp_scale(exps[row]);
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-            d[i] = u32x4{e4m3_pair(b[2 * i], s, false), e4m3_pair(b[2 * i], s, true), e4m3_pair(b[2 * i + 1], s, false),
-                         e4m3_pair(b[2 * i + 1], s, true)};
-    }
+    for (int i = 0; i < 2; ++i)
+        r.x[i] = u32x4{e4m3_pair(b[2 * i], s, false), e4m3_pair(b[2 * i], s, true), e4m3_pair(b[2 * i + 1], s, false),
+                       e4m3_pair(b[2 * i + 1], s, true)};
+    return r;
 }
 
 }  // namespace
 
-template <typename T, bool E4M3, bool WRITE>
-__global__ __launch_bounds__(256) void kv_move_kernel(KvArgs p) {
+// T: element of the tokens (and of pages that are not e4m3)
+template <typename T, bool E4M3>
+__global__ __launch_bounds__(256) void kv_write_kernel(KvArgs p) {
     const int lane = threadIdx.x & 63;
-    const int64_t j = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int64_t j = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (j >= p.n_tok) return;
-    const KvSlot s = kv_slot(p, j, lane);
-    if (s.r < 0) return;
-    // of neighbours with one position the last is written
-    if (WRITE && (s.row < 0 || s.duplicate)) return;
     const int per_head = p.d / 16, units = p.h_kv * per_head;
+    const T* ks = reinterpret_cast<const T*>(p.k) + j * p.k_stride;
+    const T* vs = reinterpret_cast<const T*>(p.v) + j * p.v_stride;
+    Raw<T> k = {}, v = {};
+    if (lane < units) k = load_raw<T>(ks + 16 * lane), v = load_raw<T>(vs + 16 * lane);
+    const int64_t first = kv_row<true>(p, j, lane);
+    if (first < 0) return;
     for (int u0 = 0; u0 < units; u0 += 64) {
         const int u = u0 + lane, hk = u / per_head, c = u % per_head;
-        const bool active = u < units;
-        const int64_t row = s.row + ((int64_t)hk << p.pg.page_shift);
-        T* k = reinterpret_cast<T*>(p.k) + j * p.k_stride + (int64_t)16 * u;
-        T* v = reinterpret_cast<T*>(p.v) + j * p.v_stride + (int64_t)16 * u;
-        if (WRITE) {
-            write_row<T, E4M3>(p, k, p.pg.k, p.pg.k_exp, row, lane, active, per_head, c);
-            write_row<T, E4M3>(p, v, p.pg.v, p.pg.v_exp, row, lane, active, per_head, c);
-        } else if (active) {
-            read_row<T, E4M3>(p, k, p.pg.k, p.pg.k_exp, s.row < 0 ? -1 : row, c);
-            read_row<T, E4M3>(p, v, p.pg.v, p.pg.v_exp, s.row < 0 ? -1 : row, c);
+        if (u0 > 0 && u < units) k = load_raw<T>(ks + 16 * u), v = load_raw<T>(vs + 16 * u);
+        const int64_t row = first + ((int64_t)hk << p.pg.page_shift);
+        if constexpr (E4M3) {
+            uint32_t kb, vb;
+            const u32x4 kc = encode(k, per_head, kb), vc = encode(v, per_head, vb);
+            if (u >= units) continue;
+            *reinterpret_cast<u32x4*>(reinterpret_cast<uint8_t*>(p.pg.k) + row * p.d + 16 * c) = kc;
+            *reinterpret_cast<u32x4*>(reinterpret_cast<uint8_t*>(p.pg.v) + row * p.d + 16 * c) = vc;
+            if (c == 0) p.pg.k_exp[row] = (uint8_t)kb, p.pg.v_exp[row] = (uint8_t)vb;
+        } else if (u < units) {
+            store_raw(reinterpret_cast<T*>(p.pg.k) + row * p.d + 16 * c, k);
+            store_raw(reinterpret_cast<T*>(p.pg.v) + row * p.d + 16 * c, v);
         }
     }
 }
 
-template <bool WRITE>
-static hipError_t launch_kv_move(const KvArgs& a, hipStream_t st) {
-    const dim3 grid((unsigned)((a.n_tok + 3) / 4));
-    if (a.kind == KV_F32) hipLaunchKernelGGL((kv_move_kernel<float, false, WRITE>), grid, dim3(256), 0, st, a);
-    else if (a.kind == KV_BF16) hipLaunchKernelGGL((kv_move_kernel<bf16, false, WRITE>), grid, dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((kv_move_kernel<bf16, true, WRITE>), grid, dim3(256), 0, st, a);
+template <typename T, bool E4M3>
+__global__ __launch_bounds__(256) void kv_read_kernel(KvArgs p) {
+    const int lane = threadIdx.x & 63;
+    const int64_t j = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (j >= p.n_tok) return;
+    const int per_head = p.d / 16, units = p.h_kv * per_head;
+    const int64_t first = kv_row<false>(p, j, lane);
+    if (first == NO_REQUEST) return;
+    for (int u = lane; u < units; u += 64) {
+        const int hk = u / per_head, c = u % per_head;
+        const int64_t row = first + ((int64_t)hk << p.pg.page_shift);
+        Raw<T> k, v;
+        if (first == NO_PLACE) {
+            const uint32_t nan = sizeof(T) == 2 ? 0x7fc07fc0u : 0x7fc00000u;
+#pragma unroll
+            for (int i = 0; i < (int)sizeof(T); ++i) k.x[i] = v.x[i] = u32x4{nan, nan, nan, nan};
+        } else if constexpr (E4M3) {
+            const u32x4 kc = *reinterpret_cast<const u32x4*>(reinterpret_cast<const uint8_t*>(p.pg.k) + row * p.d + 16 * c);
+            const u32x4 vc = *reinterpret_cast<const u32x4*>(reinterpret_cast<const uint8_t*>(p.pg.v) + row * p.d + 16 * c);
+            const uint8_t kb = p.pg.k_exp[row], vb = p.pg.v_exp[row];
+            k = decode(kc, kb), v = decode(vc, vb);
+        } else {
+            k = load_raw<T>(reinterpret_cast<const T*>(p.pg.k) + row * p.d + 16 * c);
+            v = load_raw<T>(reinterpret_cast<const T*>(p.pg.v) + row * p.d + 16 * c);
+        }
+        store_raw(reinterpret_cast<T*>(p.k) + j * p.k_stride + (int64_t)16 * u, k);
+        store_raw(reinterpret_cast<T*>(p.v) + j * p.v_stride + (int64_t)16 * u, v);
+    }
+}
+
+template <typename T, bool E4M3>
+static hipError_t launch_kv(const KvArgs& a, bool write, hipStream_t st) {
+    const dim3 grid((unsigned)((a.n_tok + 3) / 4)), block(256);
+    if (write) hipLaunchKernelGGL((kv_write_kernel<T, E4M3>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((kv_read_kernel<T, E4M3>), grid, block, 0, st, a);
     return hipGetLastError();
 }
-hipError_t launch_kv_write(const KvArgs& a, hipStream_t st) { return launch_kv_move<true>(a, st); }
-hipError_t launch_kv_read(const KvArgs& a, hipStream_t st) { return launch_kv_move<false>(a, st); }
+static hipError_t launch_kv_kind(const KvArgs& a, bool write, hipStream_t st) {
+    switch (a.kind) {
+        case KV_F32: return launch_kv<float, false>(a, write, st);
+        case KV_BF16: return launch_kv<bf16, false>(a, write, st);
+        case KV_E4M3: return launch_kv<bf16, true>(a, write, st);
+    }
+    return hipErrorInvalidValue;
+}
+hipError_t launch_kv_write(const KvArgs& a, hipStream_t st) { return launch_kv_kind(a, true, st); }
+hipError_t launch_kv_read(const KvArgs& a, hipStream_t st) { return launch_kv_kind(a, false, st); }
 
 }  // namespace lkv

@@ -224,6 +224,32 @@ def test_write_and_read(page, hkv, d, cache, io, select):
         assert same[untouched].all()
 
 
+@pytest.mark.parametrize("cache,hkv,d", [(E4, 3, 128), (BF, 9, 128), (E4, 2, 256)])
+def test_write_and_read_many(cache, hkv, d):
+    """Thousands of tokens of ragged requests, spread over their contexts, some outside them."""
+    attn = lkv.make_attn(hkv, hkv, d, page=32, cache_dtype=cache)
+    rng = np.random.default_rng(4)
+    ctx = [5000, 1, 0, 7000] + [int(x) for x in rng.integers(1, 60, 90)]
+    new = [4001, 1, 0, 6002] + [int(rng.integers(0, c + 1)) for c in ctx[4:]]
+    C = Cache(attn, ctx)
+    pos = np.concatenate([np.sort(rng.choice(c, m, replace=False)) if m else np.zeros(0, int) for c, m in zip(ctx, new)])
+    out = np.array([7, 2000, 4001, len(pos) - 1])
+    pos[out] = [-1, 5000, 1, 10 ** 6]
+    n = len(pos)
+    _, k, v = _qkv(n + 3, 1, hkv, d, BF, 4)
+    ko, vo = (torch.full((n + 3, hkv, d), 7.0, dtype=BF, device="cuda") for _ in range(2))
+    lkv.kv_write(attn, C.pages, _i32(_cum(new)), n + 3, k, v, _i32(np.append(pos, [0, 0, 0])))
+    lkv.kv_read(attn, C.pages, _i32(_cum(new)), n + 3, ko, vo, _i32(np.append(pos, [0, 0, 0])))
+    torch.cuda.synchronize()
+    for x, o in ((k, ko), (v, vo)):
+        want = _np(x[:n])
+        if cache == E4:
+            e = np.exp2(np.clip(np.ceil(np.log2(np.abs(want).max(-1) / 448)), -100, 120))[..., None]
+            want = A.e4m3_values(A.e4m3_codes(want / e), np.log2(e[..., 0]) + 127)
+        want[out] = np.nan  # position 1 of the context of one token among them
+        assert np.array_equal(_np(o[:n]), want, equal_nan=True) and bool((o[n:] == 7.0).all())
+
+
 def test_write_drops_and_duplicates():
     """Positions outside the context and pages outside the pool are dropped, and read as NaN; of
     neighbours with one position the last is written; rows behind the batch stay."""
