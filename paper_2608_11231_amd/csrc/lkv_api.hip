@@ -601,51 +601,64 @@ AttnArgs attn_args(const lkv_attn* A, const int32_t* cu, int32_t n_req, int64_t 
     return a;
 }
 
-// Launches of a call: its requests of few rows and the others each have a kernel, where the requests
-// can be of either kind.  The lengths are on the device, so the host goes by their mean: up to 32 rows
-// the few-row kernel takes all (a longer request among them just has more tiles), above it each
-// takes its own (100 decoding requests beside a chunk of 512 tokens), of one request only the tiles.
+// Launches of a call.  The lengths are on the device, so the host goes by the mean number of rows per
+// request.  Up to 16 the few-row kernel takes all (a longer request among them just has more tiles):
+// it reads 32 contexts of 8K, 8 heads of 128, in 99 us in e4m3 and 187 in bf16, the tiles in 166 and
+// 192.  Up to 32 it takes small batches, whose time is the latency of one workgroup (two contexts
+// of 4K: 18.2 us against 19.3; four of 32K in e4m3 57 against 90; 2 heads of 256 keep few workgroups
+// busy, so the tiles catch up sooner: two of 4K 22 against 25, eight of 8K 38 against 34).  All else
+// is the tiles', which overlap their short and long requests (100 single tokens and a chunk of 512 over
+// 4K in bf16: 339 us; with a kernel for either 432).  Only with e4m3 the conversion of each key for
+// few rows costs more than that overlap gains, and requests of up to 32 rows get their own kernel
+// (the same, heads of 64: 214 against 283 us; a chunk of 2048 beside 30 tokens of 8K, heads of 128: 413
+// against 477; with heads of 256, where its 32 rows fill a CU, 338 against 280: not there).
 struct AttnPlan {
-    int few_rows;   // row tile of attn_few_kernel, 0: not launched
-    int few_units;  // (request, row tile) pairs at most
+    int few_rows;    // row tile of attn_few_kernel, 0: not launched
+    int few_units;   // (request, row tile) pairs at most
     int tile_units;  // of the tile kernels, 0: not launched
     int splits;
 };
 constexpr int FEW_ROWS = 32;
 AttnPlan attn_plan(const lkv_attn* A, int32_t n_req, int64_t n_tok, bool paged, int32_t max_pages) {
     AttnPlan p = {};
-    const int64_t rows = n_tok * (A->h_q / A->h_kv);
+    const int64_t rows = n_tok * (A->h_q / A->h_kv), heads = (int64_t)n_req * A->h_kv;
     const int tile = A->io_dtype == LKV_F32 ? ATTN_ROWS_F32 : ATTN_ROWS;
     auto units = [&](int tile_rows) { return (int)(n_req + (rows - 1) / tile_rows); };
     p.splits = 1;
     if (!paged || A->io_dtype == LKV_F32) {
         p.tile_units = units(tile);
         if (!paged) return p;
-    } else if (rows <= FEW_ROWS * (int64_t)n_req) {
-        p.few_rows = rows <= 16 * (int64_t)n_req ? 16 : 32;
-        p.few_units = units(p.few_rows);
+    } else if (rows <= 16 * (int64_t)n_req) {
+        p.few_rows = 16;
+        p.few_units = units(16);
+    } else if (rows <= FEW_ROWS * (int64_t)n_req && heads <= (A->d == 256 ? 8 : 128)) {
+        p.few_rows = FEW_ROWS;
+        p.few_units = units(FEW_ROWS);
     } else {
         p.tile_units = units(tile);
-        if (n_req > 1) {
-            p.few_rows = 32;
+        if (n_req > 1 && A->d <= 128 && A->cache_dtype == LKV_E4M3) {
+            p.few_rows = FEW_ROWS;
             p.few_units = n_req;  // one tile each
         }
     }
     // Parts of the key range, none below 256 keys of the longest context.  Few rows: where the
-    // requests leave CUs idle, one round of the 512 workgroups that the GPU holds (four contexts of 8K,
-    // 8 heads: 28.7 us with 16 parts, 31.9 with 33); else more and smaller workgroups, so that the
-    // longest contexts do not end alone (128 of 1K-8K: 264 us whole, 250 in 2, 246 in 4, 274 in 8
-    // parts).  Many rows: two workgroups per CU (two chunks
-    // of 512 tokens, 130 workgroups: 430 us in 4 parts, 448 in 8, whose results cost more to join).
-    int64_t s = 1;
+    // requests leave CUs idle, one round of the workgroups that the GPU holds (four contexts of 8K,
+    // 8 heads: 28.4 us with 16 parts, 30.1 with 32); else more and smaller workgroups, so that the
+    // longest contexts do not end alone (48 of 1K-8K, 8 heads of 128: 213 us whole, 173 in 6; 128: 467
+    // whole, 433 in 2), but of 1024 keys at least, below which a part's start and its join cost more
+    // (128 of 1K: 70 us in 4, 44 whole).  Many rows: two workgroups per CU (two chunks of 512
+    // tokens, 130 workgroups: 459 us in 2 parts, 302 in 4, 299 in 8, whose workspace is twice that).
+    int64_t s = 1, part = 256;
     if (p.tile_units == 0) {
-        const int64_t wgs = (rows < (int64_t)n_req * p.few_rows ? n_req : p.few_units) * (int64_t)A->h_kv;
-        s = wgs <= 256 ? 512 / wgs : (4096 + wgs - 1) / wgs;
+        const int64_t wgs = (rows <= (int64_t)n_req * p.few_rows ? n_req : p.few_units) * (int64_t)A->h_kv;
+        const int64_t held = A->d == 256 && p.few_rows == 32 ? 256 : 512;
+        s = wgs <= held / 2 ? held / wgs : (2048 + wgs - 1) / wgs;
+        if (wgs > held / 2) part = 1024;
     } else {
         const int64_t wgs = (int64_t)p.tile_units * A->h_kv;
         if (wgs < 512) s = (512 + wgs - 1) / wgs;
     }
-    const int64_t most = ((int64_t)max_pages * A->page + 255) / 256;
+    const int64_t most = ((int64_t)max_pages * A->page + part - 1) / part;
     s = s < most ? s : most;
     p.splits = (int)(s < 1 ? 1 : (s > 128 ? 128 : s));
     return p;

@@ -386,6 +386,27 @@ def test_paged_mixed_batch(hq, hkv, d, cache):
     _check_paged(attn, C, new, q, _attn_paged(attn, C, _cum(new), q))
 
 
+@pytest.mark.parametrize("n_req", [4, 70])
+@pytest.mark.parametrize("hq,hkv,d,cache", [(8, 2, 64, BF), (8, 2, 128, E4), (16, 2, 256, BF), (16, 2, 256, E4)])
+def test_paged_drafted_tokens(n_req, hq, hkv, d, cache):
+    """Small and large batches of a few tokens each, 17 to 32 rows of a group on average, one chunk among
+    them in the large one, one long context whose keys are split."""
+    attn = lkv.make_attn(hq, hkv, d, page=16, cache_dtype=cache)
+    g = hq // hkv
+    new = [(17, 40, 24, 30)[i % 4] // g for i in range(n_req)]
+    ctx = [new[i] + 13 * i % 90 for i in range(n_req)]
+    ctx[1] += 2500
+    if n_req > 4:
+        new[9] = ctx[9] = 120 // g
+    assert 16 * n_req < g * sum(new) <= 32 * n_req
+    C = Cache(attn, ctx)
+    C.fill()
+    q = _qkv(sum(new) + 1, hq, 1, d, BF, 6)[0]
+    o = _attn_paged(attn, C, _cum(new), q)
+    _check_paged(attn, C, new, q, o)
+    assert bool((o[sum(new):] == 7.0).all())
+
+
 def test_far_offsets():
     """Rows and pages whose byte offsets pass 32 bits."""
     n, far = 530, 1 << 22  # 530 rows 2^22 elements apart: 4.4 GB
