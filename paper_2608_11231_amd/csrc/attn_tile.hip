@@ -74,7 +74,7 @@ __device__ __forceinline__ bf16x4 tr_read(uint32_t at) {
 // last key seen repeat it.  bf16 rows go from memory straight to LDS (a wave's 64 pieces land in
 // consecutive chunks, so each lane fetches the piece that belongs to its chunk); e4m3 rows pass
 // through registers, where they become bf16.
-template <int D, int KIND, bool PAGED, int BN, bool V>
+template <int D, int KIND, bool PAGED, int BN, int STEP, bool V>
 struct Stage {
     static constexpr int C = D / 8;                         // chunks of a bf16 row
     static constexpr int U = KIND == KV_E4M3 ? D / 16 : C;  // pieces of a stored row
@@ -138,7 +138,7 @@ struct Stage {
                 __builtin_amdgcn_global_load_lds((global_t*)(b + (uint32_t)o), (lds_t*)(lds + wave * 64 + i * 64 * NW), 16, 0, 0);
             }
         }
-        if (!PAGED) base += BN * stride * 2;
+        if (!PAGED) base += STEP * stride * 2;
     }
     // e4m3: the fetched tile into the buffer at byte offset `lds`.  The thread's pieces are a multiple of 16
     // rows apart, where the chunks' permutation repeats.
@@ -158,14 +158,19 @@ struct Stage {
     }
 };
 
-template <int D, int KIND, bool PAGED>
-__global__ __launch_bounds__(64 * NW, 2) void attn_tile_kernel(AttnArgs p) {
+// KG = 2: two groups of NW waves work on the same rows, each on every other tile of keys with buffers, a
+// softmax and an output of its own, joined at the end: where a call has few workgroups, the longest
+// one's chain of tiles is its time.
+template <int D, int KIND, bool PAGED, int KG>
+__global__ __launch_bounds__(64 * NW * KG, 2) void attn_tile_kernel(AttnArgs p) {
     constexpr int BN = D == 256 ? 32 : 64;  // keys of a tile
     constexpr int NT = BN / 32, NS = D / 16, ND = D / 32, C = D / 8;
-    constexpr int CHUNKS = BN * C, BM = ATTN_ROWS;
+    constexpr int CHUNKS = BN * C, BM = ATTN_ROWS, STEP = KG * BN;  // STEP: keys of a round
     static_assert(BM == 32 * NW, "a wave owns 32 rows");
-    __shared__ __align__(512) u32x4 sk[2 * CHUNKS], sv[2 * CHUNKS];  // the fragments' offsets are combined by exclusive or
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    __shared__ __align__(512) u32x4 smem[KG * 4 * CHUNKS];  // the fragments' offsets are combined by exclusive or
+    const int kg = KG == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / (64 * NW));
+    const int tid = threadIdx.x % (64 * NW), lane = tid & 63, wave = tid >> 6;  // in the group
+    u32x4 *const sk = smem + kg * 4 * CHUNKS, *const sv = sk + 2 * CHUNKS;
     const int col = lane & 31, h = lane >> 5;
 
     int b = blockIdx.x;
@@ -195,11 +200,13 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_tile_kernel(AttnArgs p) {
     all = __builtin_amdgcn_readfirstlane(all);
     const KeyRange range = key_range<BN>(end, PAGED ? p.splits : 1, split);
 
-    Stage<D, KIND, PAGED, BN, false> keys(p, w, hk, end, tid);
-    Stage<D, KIND, PAGED, BN, true> vals(p, w, hk, end, tid);
-    const int tiles = (range.to - range.from + BN - 1) / BN;
-    const int clear = min(max(all - range.from, 0) / BN, tiles);  // that every row of the workgroup sees whole
-    auto start = [&](int j) INLINE { return range.from + j * BN; };
+    Stage<D, KIND, PAGED, BN, STEP, false> keys(p, w, hk, end, tid);
+    Stage<D, KIND, PAGED, BN, STEP, true> vals(p, w, hk, end, tid);
+    const int tiles = (range.to - range.from + STEP - 1) / STEP;  // of each group
+    const int clear = min(max(all - range.from, 0) / STEP, tiles);  // that every row of the workgroup sees whole
+    auto start = [&](int j) INLINE { return range.from + j * STEP + kg * BN; };
+    // The second group's last tile may lie past the keys: it is not fetched, and masked whole
+    auto exists = [&](int j) INLINE { return j < tiles && (KG == 1 || start(j) < end); };
     int b0 = 0, b1 = CHUNKS * 16;  // buffers of the tile at hand and of the next one
     auto k_buf = [&](int o) INLINE { return reinterpret_cast<u32x4*>(reinterpret_cast<char*>(sk) + o); };
     auto v_buf = [&](int o) INLINE { return reinterpret_cast<u32x4*>(reinterpret_cast<char*>(sv) + o); };
@@ -209,12 +216,12 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_tile_kernel(AttnArgs p) {
         return p.pg.table[(int64_t)w.r * p.pg.max_pages + (j >> p.pg.page_shift)];
     };
     int ids = 0;  // pages of the next tile to fetch
-    if (tiles > 0) {
-        ids = load_ids(range.from);
-        keys.begin(range.from);
-        vals.begin(range.from);
-        keys.fetch(range.from, sk, ids);
-        vals.fetch(range.from, sv, ids);
+    if (exists(0)) {
+        ids = load_ids(start(0));
+        keys.begin(start(0));
+        vals.begin(start(0));
+        keys.fetch(start(0), sk, ids);
+        vals.fetch(start(0), sv, ids);
         ids = load_ids(start(1));
     }
 
@@ -235,7 +242,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_tile_kernel(AttnArgs p) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) ot[t][i] = 0.f;
     float m = -INFINITY, l = 0.f;  // reference of the exponents (base 2, see below) and this half's sum
-    if (tiles > 0) {
+    if (exists(0)) {
         keys.commit(lds_offset(sk));
         vals.commit(lds_offset(sv));
     }
@@ -257,7 +264,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_tile_kernel(AttnArgs p) {
     int my_pos = 0;  // set for the masked tiles
     // Tile j, whose keys and values are in the buffers at b0; the next one's are sent for.
     auto tile = [&](bool masked, int j) INLINE {
-        const bool more = j + 1 < tiles;
+        const bool more = exists(j + 1);
         if (more) {
             keys.fetch(start(j + 1), k_buf(b1), ids);
             if (KIND != KV_E4M3) {
@@ -388,10 +395,37 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_tile_kernel(AttnArgs p) {
     const AttnRow row = my_row();
     my_pos = row.kind == ROW_SEES ? row.pos : 0x7fffffff;
     for (; j < tiles; ++j) {
-        if (tid == 0) s_bad[j & 1] = 0;
+        if (threadIdx.x == 0) s_bad[j & 1] = 0;
         arrive();
         check_values(j);
         tile(true, j);
+    }
+    if constexpr (KG == 2) {  // the second group's results, through LDS, lane by lane
+        float* const so = reinterpret_cast<float*>(smem) + (wave * ND * 4 * 64 + lane) * 4;
+        __shared__ float s_m[64 * NW], s_l[64 * NW];
+        __syncthreads();
+        if (kg == 1) {
+            s_m[tid] = m, s_l[tid] = l;
+#pragma unroll
+            for (int t = 0; t < ND; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    *reinterpret_cast<f32x4*>(so + (4 * t + i) * 256) =
+                        f32x4{ot[t][4 * i], ot[t][4 * i + 1], ot[t][4 * i + 2], ot[t][4 * i + 3]};
+        }
+        __syncthreads();
+        if (kg == 1) return;
+        const float top = fmaxf(m, s_m[tid]), m_use = top == -INFINITY ? 0.f : top;
+        const float f0 = __builtin_amdgcn_exp2f(m - m_use), f1 = __builtin_amdgcn_exp2f(s_m[tid] - m_use);
+        l = f0 * l + f1 * s_l[tid];
+#pragma unroll
+        for (int t = 0; t < ND; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const f32x4 x = *reinterpret_cast<const f32x4*>(so + (4 * t + i) * 256);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) ot[t][4 * i + e] = f0 * ot[t][4 * i + e] + f1 * x[e];
+            }
     }
     const bool lost = PAGED && __syncthreads_or(keys.bad_page || vals.bad_page);  // an invalid page was read
     if (row.kind == ROW_NONE) return;
@@ -433,10 +467,18 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_tile_kernel(AttnArgs p) {
 
 template <int D>
 static hipError_t launch_d(int kind, bool paged, const AttnArgs& a, hipStream_t st) {
-    const dim3 grid((unsigned)((int64_t)a.n_units * a.h_kv * (paged ? a.splits : 1))), block(64 * NW);
-    if (!paged) hipLaunchKernelGGL((attn_tile_kernel<D, KV_BF16, false>), grid, block, 0, st, a);
-    else if (kind == KV_E4M3) hipLaunchKernelGGL((attn_tile_kernel<D, KV_E4M3, true>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((attn_tile_kernel<D, KV_BF16, true>), grid, block, 0, st, a);
+    const int64_t wgs = (int64_t)a.n_units * a.h_kv * (paged ? a.splits : 1);
+    const dim3 grid((unsigned)wgs), block(64 * NW);
+    // Two groups where the launch does not fill the GPU with workgroups, two a CU, and the chains are
+    // long (a prompt of 4096, 8 heads of 128: 89 -> 71 us; 2048, 16/2 heads of 256: 113 -> 90; filled, or
+    // short, the join and the rounds in step cost more: 16384, 8 heads of 128, 553 -> 607, 300, 16/2
+    // heads of 256, 23 -> 28).  Paged calls split their keys over workgroups instead.
+    const int64_t mean = a.n_tok / a.n_req;
+    const bool two = !paged && wgs <= (mean >= 2048 ? 512 : 256) && mean >= 1024;
+    if (two) hipLaunchKernelGGL((attn_tile_kernel<D, KV_BF16, false, 2>), grid, dim3(128 * NW), 0, st, a);
+    else if (!paged) hipLaunchKernelGGL((attn_tile_kernel<D, KV_BF16, false, 1>), grid, block, 0, st, a);
+    else if (kind == KV_E4M3) hipLaunchKernelGGL((attn_tile_kernel<D, KV_E4M3, true, 1>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((attn_tile_kernel<D, KV_BF16, true, 1>), grid, block, 0, st, a);
     return hipGetLastError();
 }
 

@@ -146,6 +146,31 @@ def test_prefill_scale_and_large_scores():
     _close(o, A.attention(_np(q), _np(k), _np(v), np.arange(400), 1.75))
 
 
+@pytest.mark.parametrize("lens", [(1024,), (1025, 1087), (1100,), (1153, 1, 2000), (2049,)], ids=str)
+@pytest.mark.parametrize("hq,hkv,d", [(2, 2, 64), (4, 1, 128), (4, 2, 256)])
+def test_prefill_of_few_long_sequences(hq, hkv, d, lens):
+    """Launches of few workgroups, with an odd and an even number of key tiles; NaN and infinities
+    behind a token change nothing of it, bit for bit."""
+    attn = lkv.make_attn(hq, hkv, d)
+    cu, n = _cum(lens), sum(lens)
+    q, k, v = _qkv(n + 2, hq, hkv, d, BF, seed=n)
+    o, o2 = (torch.full((n + 2, hq, d), 7.0, dtype=BF, device="cuda") for _ in range(2))
+    lkv.attn_prefill(attn, _i32(cu), n + 2, q, k, v, o)
+    k2, v2 = k.clone(), v.clone()
+    first = [b - 1 - (b - a) // 3 for a, b in zip(cu[:-1], cu[1:])]
+    for x in first:
+        k2[x] = float("inf")
+        v2[x] = float("nan")
+    lkv.attn_prefill(attn, _i32(cu), n + 2, q, k2, v2, o2)
+    torch.cuda.synchronize()
+    for a, b, x in zip(cu[:-1], cu[1:], first):
+        rows = np.unique(np.r_[a:min(a + 3, b), np.arange(a, b, 29), max(a, b - 140):b])
+        ref = A.attention(_np(q[rows]), _np(k[a:b]), _np(v[a:b]), rows - a, attn.scale)
+        _close(o[torch.from_numpy(rows).cuda()], ref, False, b - a, d)
+        assert torch.equal(o[a:x], o2[a:x]) and not bool(o2[x:b].isfinite().any())
+    assert bool((o[n:] == 7.0).all()) and bool((o2[n:] == 7.0).all())
+
+
 @pytest.mark.parametrize("io", [BF, F32], ids=["bf16", "f32"])
 @pytest.mark.parametrize("hq,hkv,d", [(4, 1, 64), (2, 2, 128)])
 def test_unseen_keys_do_not_matter(hq, hkv, d, io):
