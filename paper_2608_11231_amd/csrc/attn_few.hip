@@ -245,7 +245,7 @@ __global__ __launch_bounds__(64 * NW, D * RT == 512 ? 1 : 2) void attn_few_kerne
             top = fmaxf(top, __shfl_xor(top, 16));
             top = fmaxf(top, __shfl_xor(top, 32)) * p.scale_log2;
             if (__any(!(top <= m[n] + 8.f))) {  // as in attn_tile.hip
-                const float m_new = fmaxf(m[n], top);
+                const float m_new = top > m[n] + 8.f ? top : m[n];
                 const float scale = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[n] - m_new);
                 m[n] = m_new;
                 l[n] *= scale;

@@ -302,7 +302,7 @@ __global__ __launch_bounds__(64 * NW * KG, 2) void attn_tile_kernel(AttnArgs p) 
             for (int e = 0; e < 16; ++e) top = fmaxf(top, st[t][e]);
         top = half_max(top) * p.scale_log2;
         if (__any(!(top <= m + 8.f))) {
-            const float m_new = fmaxf(m, top);
+            const float m_new = top > m + 8.f ? top : m;  // by the row's own scores alone
             const float scale = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - m_new);
             m = m_new;
             l *= scale;

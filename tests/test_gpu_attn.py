@@ -467,6 +467,30 @@ def test_far_offsets():
         _close(om, A.attention(_np(q), _np(small[1]), _np(small[2]), np.arange(n - m, n), attn.scale))
 
 
+@pytest.mark.parametrize("call", ["prefill", "paged"])
+def test_rows_are_independent(call):
+    """A large score of one token leaves the sums of the others, in the same tile of rows, as they are:
+    their results are the same bits."""
+    h, d, c, n_seq, m, x = 32, 128, 300, 40, 8, 295
+    attn = lkv.make_attn(h, h, d, page=16)
+    q, k, v = _qkv(n_seq * c, h, h, d, BF, 11, False)
+    outs, at = [], torch.arange(n_seq, device="cuda") * c + x
+    C = Cache(attn, [c] * n_seq)
+    for _ in range(2):
+        if call == "prefill":
+            o = torch.empty_like(q)
+            lkv.attn_prefill(attn, _i32(np.arange(n_seq + 1) * c), n_seq * c, q, k, v, o)
+            outs.append(o.view(n_seq, c, h, d)[:, :x])
+        else:
+            lkv.kv_write(attn, C.pages, _i32(np.arange(n_seq + 1) * c), n_seq * c, k, v)
+            last = q.view(n_seq, c, h, d)[:, c - m:].reshape(n_seq * m, h, d)
+            o = _attn_paged(attn, C, np.arange(n_seq + 1) * m, last)
+            outs.append(o.view(n_seq, m, h, d)[:, :x - (c - m)])
+        k[at] *= 30
+    torch.cuda.synchronize()
+    assert torch.equal(*outs)
+
+
 # ---------------------------------------------------------------- together
 @pytest.mark.parametrize("cache", [BF, E4], ids=["bf16", "e4m3"])
 def test_reuse_flow(cache):
