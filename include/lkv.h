@@ -391,7 +391,9 @@ lkv_status lkv_state_rel_error(const float* S, const float* S_ref, int32_t n_sli
  * bytes, at least heads * d, at most 2^22), so q, k and v may be views of one
  * projection's output; o is dense.  cu: device int32 [n_req+1], cu[0] = 0, non-decreasing;
  * n_tok: host bound of cu[n_req].  Rows from cu[n_req] on are not touched, so
- * a padded batch (a captured graph's) may pass its capacity. */
+ * a padded batch (a captured graph's) may pass its capacity.  A call whose launch
+ * would pass 2^24 workgroups is refused (LKV_E_SHAPE): 2^26 tokens of a write or
+ * read, 2^28 rows (tokens * h_q) of attention for short requests and for fp32. */
 typedef struct {
     int32_t h_q;
     int32_t h_kv;

@@ -3,6 +3,7 @@
 #include <math.h>
 #include <stdlib.h>
 
+#include <algorithm>
 #include <atomic>
 #include <mutex>
 
@@ -549,6 +550,9 @@ lkv_status check_counts(const lkv_attn* A, int32_t n_req, int64_t n_tok) {
     return LKV_OK;
 }
 
+// A launch's threads stay below 2^32
+bool launches(int64_t wgs) { return wgs < 1 << 24; }
+
 // rows of `heads` heads, `stride` elements apart
 lkv_status check_rows(const lkv_attn* A, const void* x, int64_t stride, int32_t heads) {
     if (!x) return LKV_E_NULL;
@@ -686,6 +690,7 @@ lkv_status kv_move(const lkv_attn* A, const lkv_pages* P, const int32_t* cu, int
     s = check_rows(A, k, k_stride, A->h_kv);
     if (s == LKV_OK) s = check_rows(A, v, v_stride, A->h_kv);
     if (s != LKV_OK) return s;
+    if (!launches((n_tok + 3) / 4)) return LKV_E_SHAPE;
     KvArgs a = {};
     a.cu = cu;
     a.n_req = n_req;
@@ -961,6 +966,7 @@ lkv_status lkv_attn_prefill(const lkv_attn* A, const int32_t* cu, int32_t n_seq,
     a.k_stride = k_stride;
     a.v_stride = v_stride;
     a.n_units = attn_plan(A, n_seq, n_tok, false, 0).tile_units;
+    if (!launches((int64_t)a.n_units * A->h_kv)) return LKV_E_SHAPE;
     a.splits = 1;
     hipStream_t st = (hipStream_t)stream;
     return hip_status(A->io_dtype == LKV_F32 ? launch_attn_f32(A->d, false, a, st) : launch_attn(A->d, KV_BF16, false, a, st));
@@ -1002,6 +1008,9 @@ lkv_status lkv_attn_paged(const lkv_attn* A, const lkv_pages* P, const int32_t* 
     a.pg = pages_args(A, P);
     const AttnPlan plan = attn_plan(A, n_req, n_tok, true, P->max_pages);
     a.splits = plan.splits;
+    if (!launches((int64_t)std::max(plan.tile_units, plan.few_units) * A->h_kv * a.splits) ||
+        (a.splits > 1 && !launches(n_tok * A->h_q)))
+        return LKV_E_SHAPE;
     const AttnWs w = attn_ws(A, n_tok, a.splits);
     if (w.total > 0) {
         if (!ws) return LKV_E_NULL;

@@ -337,6 +337,8 @@ def make_attn(h_q: int, h_kv: int, d: int, scale: Optional[float] = None, page: 
     ``io_dtype``, and is ``torch.float8_e4m3fn`` for a quantised cache."""
     cache = dtype_code(io_dtype) if cache_dtype is None else (
         E4M3 if cache_dtype == torch.float8_e4m3fn else dtype_code(cache_dtype))
+    if min(h_q, h_kv, d) < 1:
+        raise ValueError("make_attn: h_q, h_kv and d must be positive")
     a = Attn(h_q, h_kv, d, page, dtype_code(io_dtype), cache, d ** -0.5 if scale is None else scale)
     a._io, a._d, a._hq, a._hkv = io_dtype, d, h_q, h_kv
     a._cache = {F32: torch.float32, BF16: torch.bfloat16, E4M3: torch.float8_e4m3fn}[cache]

@@ -87,6 +87,22 @@ def test_paged_arguments():
     assert _moves(a, _pages(), ks=248) == _moves(a, _pages(), vs=248) == SHAPE
 
 
+def test_too_many_workgroups():
+    """Launches past 2^24 workgroups are refused, on whichever grid is the large one."""
+    a, one = _attn(), _attn(h_q=1, h_kv=1)
+    assert _moves(one, _pages(), n_tok=1 << 26) == SHAPE
+    assert _prefill(one, n_tok=(1 << 31) - 1, qs=128, ks=128, vs=128) == SHAPE
+    assert _prefill(one, n_seq=1 << 24, n_tok=1, qs=128, ks=128, vs=128) == SHAPE
+    assert _paged(a, _pages(max_pages=1), n_req=1 << 23, n_tok=1 << 23) == SHAPE
+    assert _paged(one, _pages(max_pages=1), n_req=1 << 26, n_tok=1 << 30, qs=128) == SHAPE
+
+
+@pytest.mark.parametrize("bad", [(0, 2, 128), (8, 0, 128), (8, 2, 0), (8, 2, -64)], ids=str)
+def test_make_attn_of_nothing(bad):
+    with pytest.raises(ValueError):
+        lkv.make_attn(*bad)
+
+
 def test_workspace():
     a = _attn()
     need = lkv.attn_paged_workspace(a, 1, 4, 512)  # one request, a long context: split
