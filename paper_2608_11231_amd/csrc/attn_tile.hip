@@ -12,8 +12,8 @@
 // for the product (2^-8 of each at most, as the outputs are).
 //
 // Power bounds the large calls (two workgroups per CU: the clock falls to 2.0 GHz with the matrix
-// cores half busy): a 32K prompt of 32/8 heads of 128 takes 8.3 to 8.5 ms, 1.05 PFLOP/s; an 8K
-// prompt of 16/2 heads of 256 0.53 to 0.58 ms, 1.0 PFLOP/s.  Measured beside it and not better: the
+// cores half busy): a 32K prompt of 32/8 heads of 128 takes 8.1 to 8.5 ms, 1.06 PFLOP/s; an 8K
+// prompt of 16/2 heads of 256 0.51 to 0.58 ms, 1.0 PFLOP/s.  Measured beside it and not better: the
 // next tile's scores formed in between softmax and product (8.3 ms), eight waves that share a tile
 // (8.4), three waves per SIMD on tiles of 32 keys (8.2; 32 ragged blocks 490 against 460 us), keys
 // staged through registers (8.0 with eight waves, but paged keys 6.2 against 4.7 ms), 64 rows per

