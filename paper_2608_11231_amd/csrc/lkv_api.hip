@@ -623,6 +623,7 @@ struct AttnPlan {
     int splits;
 };
 constexpr int FEW_ROWS = 32;
+constexpr int64_t MAX_PARTS = 128;  // that the join takes
 AttnPlan attn_plan(const lkv_attn* A, int32_t n_req, int64_t n_tok, bool paged, int32_t max_pages) {
     AttnPlan p = {};
     const int64_t rows = n_tok * (A->h_q / A->h_kv), heads = (int64_t)n_req * A->h_kv;
@@ -650,21 +651,33 @@ AttnPlan attn_plan(const lkv_attn* A, int32_t n_req, int64_t n_tok, bool paged, 
     // 8 heads: 28.4 us with 16 parts, 30.1 with 32); else more and smaller workgroups, so that the
     // longest contexts do not end alone (48 of 1K-8K, 8 heads of 128: 213 us whole, 173 in 6; 128: 467
     // whole, 433 in 2), but of 1024 keys at least, below which a part's start and its join cost more
-    // (128 of 1K: 70 us in 4, 44 whole).  Many rows: two workgroups per CU (two chunks of 512
-    // tokens, 130 workgroups: 459 us in 2 parts, 302 in 4, 299 in 8, whose workspace is twice that).
-    int64_t s = 1, part = 256;
+    // (128 of 1K: 70 us in 4, 44 whole).
+    const int64_t context = (int64_t)max_pages * A->page;
     if (p.tile_units == 0) {
         const int64_t wgs = (rows <= (int64_t)n_req * p.few_rows ? n_req : p.few_units) * (int64_t)A->h_kv;
         const int64_t held = A->d == 256 && p.few_rows == 32 ? 256 : 512;
-        s = wgs <= held / 2 ? held / wgs : (2048 + wgs - 1) / wgs;
-        if (wgs > held / 2) part = 1024;
-    } else {
-        const int64_t wgs = (int64_t)p.tile_units * A->h_kv;
-        if (wgs < 512) s = (512 + wgs - 1) / wgs;
+        const int64_t part = wgs <= held / 2 ? 256 : 1024;
+        const int64_t s = wgs <= held / 2 ? held / wgs : (2048 + wgs - 1) / wgs;
+        p.splits = (int)std::max<int64_t>(1, std::min({s, (context + part - 1) / part, MAX_PARTS}));
+        return p;
     }
-    const int64_t most = ((int64_t)max_pages * A->page + part - 1) / part;
-    s = s < most ? s : most;
-    p.splits = (int)(s < 1 ? 1 : (s > 128 ? 128 : s));
+    // Many rows: the least time, of rounds * (tiles of a part + its start) + the parts' way to the join
+    // and back (4 TB/s, and its chain of loads), over the parts that up to four rounds of 512
+    // workgroups allow, as if the requests were of one length.  Filling the rounds is what counts: 1500
+    // tokens over 32K (188 workgroups of 2 heads of 256): 1215 us in 3 parts (1.1 rounds), 806 in 8 (2.9);
+    // 2100, 8 heads of 128 (528): 1770 whole, 1264 in 4.  Launches of two rounds and more stay whole.
+    const int64_t each = (rows + n_req - 1) / n_req;
+    const int64_t wgs = std::min<int64_t>(p.tile_units, (each + tile - 1) / tile * n_req) * A->h_kv;
+    if (wgs >= 1024) return p;
+    const float tile_us = A->d == 64 ? 1.f : 2.f, start_us = 8.f;  // 64 keys, at d = 256 32
+    const float range_us = (float)context / (A->d == 256 ? 32 : 64) * tile_us;
+    const float join_us = (float)n_tok * A->h_q * A->d * 8 / 4e6f + 0.2f;
+    const int64_t most = std::min({(2048 + wgs - 1) / wgs, (context + 255) / 256, MAX_PARTS});
+    float best = INFINITY;
+    for (int64_t s = 1; s <= most; ++s) {
+        const float cost = (float)((wgs * s + 511) / 512) * (range_us / s + start_us) + (s > 1 ? s * join_us : 0.f);
+        if (cost < best) best = cost, p.splits = (int)s;
+    }
     return p;
 }
 
