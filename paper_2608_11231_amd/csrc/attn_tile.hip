@@ -19,6 +19,8 @@
 // staged through registers (8.0 with eight waves, but paged keys 6.2 against 4.7 ms), 64 rows per
 // wave with one wave per SIMD (9.4 and more: each fragment read serves two products, but nothing
 // hides the LDS and barrier waits).
+#include <algorithm>
+
 #include "attn_device.h"
 
 namespace lkv {
@@ -205,7 +207,7 @@ __global__ __launch_bounds__(64 * NW * KG, 2) void attn_tile_kernel(AttnArgs p) 
     const int tiles = (range.to - range.from + STEP - 1) / STEP;  // of each group
     const int clear = min(max(all - range.from, 0) / STEP, tiles);  // that every row of the workgroup sees whole
     auto start = [&](int j) INLINE { return range.from + j * STEP + kg * BN; };
-    // The second group's last tile may lie past the keys: it is not fetched, and masked whole
+    // The second group's last tile may lie past the keys: its values are zeros, its scores masked
     auto exists = [&](int j) INLINE { return j < tiles && (KG == 1 || start(j) < end); };
     int b0 = 0, b1 = CHUNKS * 16;  // buffers of the tile at hand and of the next one
     auto k_buf = [&](int o) INLINE { return reinterpret_cast<u32x4*>(reinterpret_cast<char*>(sk) + o); };
@@ -354,6 +356,8 @@ __global__ __launch_bounds__(64 * NW * KG, 2) void attn_tile_kernel(AttnArgs p) 
     // becomes NaN, and they are zeros from then on.
     auto check_values = [&](int j) INLINE {
         bool bad = false;
+        if (!exists(j))
+            for (int x = tid; x < CHUNKS; x += 64 * NW) v_buf(b0)[x] = u32x4{0, 0, 0, 0};
 #pragma unroll
         for (int i = 0; i < CHUNKS / (64 * NW); ++i) bad |= nonfinite_bits(v_buf(b0)[tid + i * 64 * NW]) != 0;
         if (bad) s_bad[j & 1] = 1;
@@ -470,11 +474,11 @@ static hipError_t launch_d(int kind, bool paged, const AttnArgs& a, hipStream_t 
     const int64_t wgs = (int64_t)a.n_units * a.h_kv * (paged ? a.splits : 1);
     const dim3 grid((unsigned)wgs), block(64 * NW);
     // Two groups where the launch does not fill the GPU with workgroups, two a CU, and the chains are
-    // long (a prompt of 4096, 8 heads of 128: 89 -> 71 us; 2048, 16/2 heads of 256: 113 -> 90; filled, or
-    // short, the join and the rounds in step cost more: 16384, 8 heads of 128, 553 -> 607, 300, 16/2
-    // heads of 256, 23 -> 28).  Paged calls split their keys over workgroups instead.
+    // long (a prompt of 4096, 8 heads of 128: 88 -> 68 us; 2048, 16/2 heads of 256: 116 -> 76; filled, or
+    // short, the join and the rounds in step cost more: 16384, 8 heads of 128, 553 -> 607; four of
+    // 300, 32/8 heads of 128, 15 -> 21).  Paged calls split their keys over workgroups instead.
     const int64_t mean = a.n_tok / a.n_req;
-    const bool two = !paged && wgs <= (mean >= 2048 ? 512 : 256) && mean >= 1024;
+    const bool two = !paged && mean >= 512 && wgs <= std::min<int64_t>(512, mean * 3 / 8);
     if (two) hipLaunchKernelGGL((attn_tile_kernel<D, KV_BF16, false, 2>), grid, dim3(128 * NW), 0, st, a);
     else if (!paged) hipLaunchKernelGGL((attn_tile_kernel<D, KV_BF16, false, 1>), grid, block, 0, st, a);
     else if (kind == KV_E4M3) hipLaunchKernelGGL((attn_tile_kernel<D, KV_E4M3, true, 1>), grid, block, 0, st, a);
