@@ -275,6 +275,11 @@ def test_write_and_read_many(cache, hkv, d):
         assert np.array_equal(_np(o[:n]), want, equal_nan=True) and bool((o[n:] == 7.0).all())
 
 
+@pytest.mark.parametrize("cache,hkv,d", [(E4, 1, 128), (E4, 1, 64), (BF, 2, 64), (BF, 2, 256)])
+def test_write_and_read_many_of_few_heads(cache, hkv, d):
+    test_write_and_read_many(cache, hkv, d)
+
+
 def test_write_drops_and_duplicates():
     """Positions outside the context and pages outside the pool are dropped, and read as NaN; of
     neighbours with one position the last is written; rows behind the batch stay."""
