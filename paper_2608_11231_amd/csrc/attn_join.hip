@@ -3,6 +3,8 @@
 namespace lkv {
 
 // Join of the key ranges' results: with m = max m_s, o = sum 2^(m_s - m) o_s / sum 2^(m_s - m) l_s.
+// A part in which the row sees no key has l_s = 0 and no o_s; every other one counts, also where its
+// weight underflows to 0, since 0 times a value that is not finite is NaN.
 // A workgroup joins one row: every wave forms all weights, a part per lane, and adds a quarter of
 // the parts, whose loads do not wait for each other; the quarters meet in LDS.  Short chains of
 // loads are what counts here: a decoding call waits for it (four contexts of 8K in 16 parts: 28 us
@@ -28,8 +30,10 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs p) {
     for (int i = 1; i < 64; i <<= 1) m = fmaxf(m, __shfl_xor(m, i));
     const float m_use = m == -INFINITY ? 0.f : m;
     float f[JOIN_PARTS / 64], l = 0.f;
+    uint64_t written[JOIN_PARTS / 64];
 #pragma unroll
     for (int i = 0; i < JOIN_PARTS / 64; ++i) {
+        written[i] = __ballot(ls[i] != 0.f);
         f[i] = ls[i] == 0.f ? 0.f : __builtin_amdgcn_exp2f(ms[i] - m_use);
         l += f[i] * ls[i];
     }
@@ -54,7 +58,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs p) {
                 const int s = s0 + 4 * k;
                 const float w = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, f[i]), s & 63));
 #pragma unroll
-                for (int e = 0; e < E; ++e) o[e] += s < to && w != 0.f ? w * y[k][e] : 0.f;  // parts without keys are not written
+                for (int e = 0; e < E; ++e) o[e] += s < to && (written[i] >> (s & 63)) & 1 ? w * y[k][e] : 0.f;
             }
         }
     }
@@ -96,6 +100,7 @@ __global__ __launch_bounds__(256) void attn_join_rows_kernel(AttnArgs p) {
 #pragma unroll
     for (int i = 1; i < 64; i <<= 1) top = fmaxf(top, __shfl_xor(top, i));
     const float f = l == 0.f ? 0.f : __builtin_amdgcn_exp2f(m - (top == -INFINITY ? 0.f : top));
+    const uint64_t written = __ballot(l != 0.f);  // no bits past the last part
     l *= f;
 #pragma unroll
     for (int i = 1; i < 64; i <<= 1) l += __shfl_xor(l, i);
@@ -107,9 +112,8 @@ __global__ __launch_bounds__(256) void attn_join_rows_kernel(AttnArgs p) {
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             const float w = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, f), s0 + k));
-            // lanes past the last part have weight 0; parts without keys are not written
 #pragma unroll
-            for (int e = 0; e < E; ++e) o[e] += w != 0.f ? w * y[k][e] : 0.f;
+            for (int e = 0; e < E; ++e) o[e] += (written >> (s0 + k)) & 1 ? w * y[k][e] : 0.f;
         }
     }
     const float inv = 1.f / l;

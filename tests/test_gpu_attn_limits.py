@@ -1,0 +1,67 @@
+"""The full-attention calls at the limits of what they take: values that are infinite or NaN under weights
+that vanish."""
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+if not torch.cuda.is_available():
+    pytest.skip("no GPU", allow_module_level=True)
+
+from paper_2608_11231_amd import lkv  # noqa: E402
+from test_gpu_attn import BF, E4, F32, Cache, _attn_paged, _i32, _qkv  # noqa: E402
+
+# name: h_q, h_kv, d, io, cache, context, new tokens; by `parts` the call's key range is split
+SPLIT = {
+    "one_token_8_parts": (8, 2, 128, BF, BF, 2000, 1),
+    "one_token_36_parts": (8, 2, 128, BF, BF, 9000, 1),
+    "drafted_e4m3": (8, 2, 64, BF, E4, 9000, 8),
+    "drafted_wide": (8, 2, 256, BF, BF, 9000, 8),
+    "chunk": (8, 2, 128, BF, BF, 9000, 60),
+    "chunk_many_rows": (8, 2, 64, BF, E4, 9000, 300),
+    "chunk_wide_e4m3": (8, 2, 256, BF, E4, 9000, 60),
+    "f32_7_parts": (4, 2, 64, F32, F32, 1700, 3),
+    "f32_many_parts": (4, 2, 128, F32, F32, 9000, 3),
+}
+WHOLE = {
+    "one_token_whole": (8, 2, 128, BF, BF, 200, 1),
+    "chunk_whole": (8, 2, 256, BF, BF, 200, 60),
+    "f32_whole": (4, 2, 64, F32, F32, 200, 3),
+}
+BOTH = {**SPLIT, **WHOLE}
+
+
+def _layer(name):
+    hq, hkv, d, io, cache, ctx, new = BOTH[name]
+    attn = lkv.make_attn(hq, hkv, d, page=16, io_dtype=io, cache_dtype=cache)
+    width = -(-ctx // 16) + 1
+    assert (lkv.attn_paged_workspace(attn, 1, new, width) > 0) == (name in SPLIT)
+    q, k, v = _qkv(ctx, hq, hkv, d, io, 7, False)
+    q = q[:new].contiguous()
+    q[:, :, 0], k[:, :, 0] = 8.0, 0.0
+    return attn, Cache(attn, [ctx]), q, k, v, ctx, new
+
+
+def _over(attn, C, q, k, v):
+    n = k.shape[0]
+    lkv.kv_write(attn, C.pages, _i32([0, n]), n, k, v)
+    return _attn_paged(attn, C, [0, q.shape[0]], q)
+
+
+def _same_but(good, bad, channels):
+    """`bad` is not finite in these channels and `good`'s bits in the others."""
+    rest = [c for c in range(good.shape[-1]) if c not in channels]
+    assert bool(good.isfinite().all())
+    assert not bool(bad[..., channels].isfinite().any())
+    assert torch.equal(good[..., rest], bad[..., rest])
+
+
+@pytest.mark.parametrize("name", BOTH)
+def test_values_of_vanishing_weight(name):
+    """An infinite or NaN value counts however small its weight is: 0 * NaN is NaN.  One late key outweighs
+    the others by 250 nats and more, past what an exponential in fp32 holds."""
+    attn, C, q, k, v, ctx, new = _layer(name)
+    k[ctx - new - 1, :, 0] = 512.0
+    good = _over(attn, C, q, k, v)
+    v[3, :, 3], v[ctx // 3, :, 7], v[ctx // 2, :, 9] = float("nan"), float("inf"), float("-inf")
+    _same_but(good, _over(attn, C, q, k, v), [3, 7, 9])
