@@ -383,10 +383,10 @@ lkv_status lkv_state_rel_error(const float* S, const float* S_ref, int32_t n_sli
  * A token at position p attends to its request's keys 0..p: with s_j = scale
  * q.k_j, o = sum_j exp(s_j) v_j / sum_j exp(s_j).  Scores, statistics and sums
  * are fp32; with bf16 tokens the probabilities are rounded to bf16 for the
- * product with v.  A token that sees no key gives zeros.  Keys and values that
- * a token does not see do not affect it, whatever they hold; if a value that it
- * sees is infinite or NaN, that element of its output is not finite, however
- * small the value's weight.
+ * product with v.  A token that sees no key gives zeros, and so does one whose
+ * scores are all -inf.  Keys and values that a token does not see do not affect
+ * it, whatever they hold; if a value that it sees is infinite or NaN, that
+ * element of its output is not finite, however small the value's weight.
  *
  * Token arrays have rows [heads, d] `stride` elements apart (a multiple of 16
  * bytes, at least heads * d, at most 2^22), so q, k and v may be views of one

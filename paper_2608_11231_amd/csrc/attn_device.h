@@ -123,6 +123,13 @@ __device__ __forceinline__ KeyRange key_range(int end, int splits, int s) {
     return KeyRange{(int)(a < end ? a : end), (int)(b < end ? b : end)};
 }
 
+// A row's sum as stored for the join.  0 says that the row sees no key of the part and that its o is not
+// written.  A row whose seen scores are all -inf has a sum of 0 too (and the reference -inf, so no weight),
+// but its o counts: NaN where a value is not finite, else 0.
+__device__ __forceinline__ float part_sum(float sum, const AttnRow& x, const KeyRange& range) {
+    return sum == 0.f && x.kind == ROW_SEES && x.pos >= range.from ? 1.f : sum;
+}
+
 // Eight bf16: bit i for an infinite or NaN element, the elements of set bits cleared, ones for set bits
 __device__ __forceinline__ uint32_t nonfinite_bits(u32x4 x) {
     uint32_t b = 0;

@@ -184,19 +184,20 @@ __global__ __launch_bounds__(64 * NW) void attn_f32_kernel(AttnArgs p) {
     if (row.kind == ROW_ZERO) l = 0.f;
     if (PAGED && p.splits > 1) {
         const int64_t at = (int64_t)split * p.n_tok * p.h_q + row.tok * p.h_q + row.head;
+        const float stored = part_sum(l, row, range);
         if (g == 0) {
             p.part_ml[2 * at] = row.kind == ROW_ZERO ? -INFINITY : m_all;
-            p.part_ml[2 * at + 1] = l;
+            p.part_ml[2 * at + 1] = stored;
         }
-        if (l == 0.f) return;
+        if (stored == 0.f) return;
 #pragma unroll
         for (int t = 0; t < ND; ++t) *reinterpret_cast<f32x4*>(p.part_o + at * D + 16 * t + 4 * g) = ot[t];
         return;
     }
-    const float inv = 1.f / l;
+    const float inv = l == 0.f ? 1.f : 1.f / l;  // as in attn_tile.hip
     float* o = reinterpret_cast<float*>(p.o) + (row.tok * p.h_q + row.head) * D;
 #pragma unroll
-    for (int t = 0; t < ND; ++t) *reinterpret_cast<f32x4*>(o + 16 * t + 4 * g) = l == 0.f ? zero4() : ot[t] * inv;
+    for (int t = 0; t < ND; ++t) *reinterpret_cast<f32x4*>(o + 16 * t + 4 * g) = row.kind == ROW_ZERO ? zero4() : ot[t] * inv;
 }
 
 hipError_t launch_attn_f32(int d, bool paged, const AttnArgs& a, hipStream_t st) {

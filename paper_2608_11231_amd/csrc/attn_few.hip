@@ -330,13 +330,14 @@ __global__ __launch_bounds__(64 * NW, D * RT == 512 ? 1 : 2) void attn_few_kerne
         if (x.kind == ROW_ZERO) total = 0.f, top = -INFINITY;
         const int64_t at = x.tok * p.h_q + x.head, pat = (int64_t)split * p.n_tok * p.h_q + at;
         if (p.splits > 1) {
+            const float stored = part_sum(total, x, range);
             if (jc == 0) {
                 p.part_ml[2 * pat] = top;
-                p.part_ml[2 * pat + 1] = total;
+                p.part_ml[2 * pat + 1] = stored;
             }
-            if (total == 0.f) continue;
+            if (stored == 0.f) continue;
         }
-        const float inv = 1.f / total;
+        const float inv = total == 0.f ? 1.f : 1.f / total;  // as in attn_tile.hip
 #pragma unroll
         for (int e = 0; e < D / 64; ++e) {
             f32x4 y = zero4();
@@ -345,7 +346,7 @@ __global__ __launch_bounds__(64 * NW, D * RT == 512 ? 1 : 2) void attn_few_kerne
             if (p.splits > 1) *reinterpret_cast<f32x4*>(p.part_o + pat * D + 64 * e + 4 * jc) = y;
             else
                 *reinterpret_cast<bf16x4*>(reinterpret_cast<bf16*>(p.o) + at * D + 64 * e + 4 * jc) =
-                    total == 0.f ? zero_bf16x4() : to_bf16(y * inv);
+                    x.kind == ROW_ZERO ? zero_bf16x4() : to_bf16(y * inv);
         }
     }
 }

@@ -4,7 +4,7 @@ namespace lkv {
 
 // Join of the key ranges' results: with m = max m_s, o = sum 2^(m_s - m) o_s / sum 2^(m_s - m) l_s.
 // A part in which the row sees no key has l_s = 0 and no o_s; every other one counts, also where its
-// weight underflows to 0, since 0 times a value that is not finite is NaN.
+// weight underflows to 0, since 0 times a value that is not finite is NaN (see part_sum).
 // A workgroup joins one row: every wave forms all weights, a part per lane, and adds a quarter of
 // the parts, whose loads do not wait for each other; the quarters meet in LDS.  Short chains of
 // loads are what counts here: a decoding call waits for it (four contexts of 8K in 16 parts: 28 us
@@ -67,12 +67,12 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs p) {
         for (int e = 0; e < E; ++e) so[wave - 1][E * lane + e] = o[e];
     __syncthreads();
     if (wave > 0) return;
-    const float inv = 1.f / l;
+    const float inv = l == 0.f ? 1.f : 1.f / l;
     T* out = reinterpret_cast<T*>(p.o) + at * D + E * lane;
 #pragma unroll
     for (int e = 0; e < E; ++e) {
         const int x = E * lane + e;
-        out[e] = (T)(l == 0.f ? 0.f : (o[e] + so[0][x] + so[1][x] + so[2][x]) * inv);
+        out[e] = (T)((o[e] + so[0][x] + so[1][x] + so[2][x]) * inv);
     }
 }
 
@@ -116,10 +116,10 @@ __global__ __launch_bounds__(256) void attn_join_rows_kernel(AttnArgs p) {
             for (int e = 0; e < E; ++e) o[e] += (written >> (s0 + k)) & 1 ? w * y[k][e] : 0.f;
         }
     }
-    const float inv = 1.f / l;
+    const float inv = l == 0.f ? 1.f : 1.f / l;
     T* out = reinterpret_cast<T*>(p.o) + at * D + E * lane;
 #pragma unroll
-    for (int e = 0; e < E; ++e) out[e] = (T)(l == 0.f ? 0.f : o[e] * inv);
+    for (int e = 0; e < E; ++e) out[e] = (T)(o[e] * inv);
 }
 
 template <int D, typename T>

@@ -433,14 +433,15 @@ __global__ __launch_bounds__(64 * NW * KG, 2) void attn_tile_kernel(AttnArgs p) 
     }
     const bool lost = PAGED && __syncthreads_or(keys.bad_page || vals.bad_page);  // an invalid page was read
     if (row.kind == ROW_NONE) return;
-    const float sum = lost || row.kind == ROW_NAN ? NAN : row.kind == ROW_ZERO ? 0.f : half_sum(l);
+    const float sum = row.kind == ROW_ZERO ? 0.f : lost || row.kind == ROW_NAN ? NAN : half_sum(l);
     if (PAGED && p.splits > 1) {
         const int64_t at = (int64_t)split * p.n_tok * p.h_q + row.tok * p.h_q + row.head;
+        const float stored = part_sum(sum, row, range);
         if (h == 0) {
             p.part_ml[2 * at] = row.kind == ROW_ZERO ? -INFINITY : m;
-            p.part_ml[2 * at + 1] = sum;
+            p.part_ml[2 * at + 1] = stored;
         }
-        if (sum == 0.f) return;  // not read
+        if (stored == 0.f) return;  // not read
 #pragma unroll
         for (int t = 0; t < ND; ++t)
 #pragma unroll
@@ -449,8 +450,9 @@ __global__ __launch_bounds__(64 * NW * KG, 2) void attn_tile_kernel(AttnArgs p) 
                     f32x4{ot[t][4 * i], ot[t][4 * i + 1], ot[t][4 * i + 2], ot[t][4 * i + 3]};
         return;
     }
-    // Two groups of four of the lane's values, exchanged between the halves, make 16 adjacent bytes
-    const float inv = 1.f / sum;
+    // Two groups of four of the lane's values, exchanged between the halves, make 16 adjacent bytes.  Where all
+    // scores are -inf the sum is 0 and O as it stands the result: 0, or NaN where a value is not finite.
+    const float inv = sum == 0.f ? 1.f : 1.f / sum;
     bf16* o = reinterpret_cast<bf16*>(p.o) + (row.tok * p.h_q + row.head) * D;
 #pragma unroll
     for (int t = 0; t < ND; ++t)
@@ -464,7 +466,7 @@ __global__ __launch_bounds__(64 * NW * KG, 2) void attn_tile_kernel(AttnArgs p) 
                                                                 pack_bf16x2(ot[t][c] * inv, ot[t][c + 1] * inv), false, false);
                 y[e] = r[0], y[2 + e] = r[1];
             }
-            if (sum == 0.f) y = u32x4{0, 0, 0, 0};
+            if (row.kind == ROW_ZERO) y = u32x4{0, 0, 0, 0};
             *reinterpret_cast<u32x4*>(o + 32 * t + 8 * i + 8 * h) = y;
         }
 }

@@ -1,5 +1,5 @@
 """The full-attention calls at the limits of what they take: values that are infinite or NaN under weights
-that vanish."""
+that vanish, scores of -inf."""
 import pytest
 
 pytestmark = pytest.mark.gpu
@@ -65,3 +65,49 @@ def test_values_of_vanishing_weight(name):
     good = _over(attn, C, q, k, v)
     v[3, :, 3], v[ctx // 3, :, 7], v[ctx // 2, :, 9] = float("nan"), float("inf"), float("-inf")
     _same_but(good, _over(attn, C, q, k, v), [3, 7, 9])
+
+
+@pytest.mark.parametrize("name", [x for x in BOTH if BOTH[x][4] != E4])
+@pytest.mark.parametrize("seen", ["half", "none"])
+def test_scores_of_minus_infinity(name, seen):
+    """Keys whose scores are -inf have no weight, and a token with no other keys gives zeros; a value among
+    them that is not finite counts all the same."""
+    attn, C, q, k, v, ctx, new = _layer(name)
+    k[:ctx // 2 if seen == "half" else ctx, :, 0] = float("-inf")
+    good = _over(attn, C, q, k, v)
+    if seen == "none":
+        assert bool((good == 0).all())
+    v[3, :, 3], v[ctx // 3, :, 7] = float("nan"), float("inf")
+    _same_but(good, _over(attn, C, q, k, v), [3, 7])
+
+
+@pytest.mark.parametrize("n", [70, 1100])
+@pytest.mark.parametrize("hq,d,io", [(2, 64, BF), (2, 128, BF), (2, 256, BF), (2, 128, F32)])
+def test_prefill_scores_of_minus_infinity(n, hq, d, io):
+    attn = lkv.make_attn(hq, 1, d, io_dtype=io)
+    q, k, v = _qkv(n, hq, 1, d, io, 5, False)
+    q[:, :, 0], k[:, :, 0] = 1.0, float("-inf")
+    outs = []
+    for _ in range(2):
+        o = torch.full_like(q, 7.0)
+        lkv.attn_prefill(attn, _i32([0, n]), n, q, k, v, o)
+        outs.append(o)
+        v[20, :, 3] = float("nan")
+    torch.cuda.synchronize()
+    assert bool((outs[0] == 0).all()) and torch.equal(outs[0][:20], outs[1][:20])
+    _same_but(outs[0][20:], outs[1][20:], [3])
+
+
+def test_a_token_without_keys_beside_values_not_finite():
+    """Tokens before the context's start give zeros, whatever their request's values hold."""
+    for new, io in ((5, BF), (60, BF), (5, F32)):
+        attn = lkv.make_attn(8, 2, 64, page=16, io_dtype=io)
+        C = Cache(attn, [3])
+        q, k, v = _qkv(new, 8, 2, 64, io, 7, False)
+        v[0] = float("nan")
+        o = torch.full_like(q, 7.0)
+        lkv.kv_write(attn, C.pages, _i32([0, 3]), 3, k, v)
+        ws = torch.empty(lkv.attn_paged_workspace(attn, 1, new, 2), dtype=torch.uint8, device="cuda")
+        lkv.attn_paged(attn, C.pages, _i32([0, new]), new, q, o, ws)
+        torch.cuda.synchronize()
+        assert bool((o[:new - 3] == 0).all()) and bool(o[new - 3:].isnan().all())
