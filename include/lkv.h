@@ -408,7 +408,8 @@ typedef struct {
 /* Paged cache of one layer.
  *   k, v     [n_page, h_kv, page, d] cache_dtype, device
  *   k_exp, v_exp  LKV_E4M3: [n_page, h_kv, page] uint8, device: a row of codes c
- *            stands for c * 2^(exp - 127), exp in [27, 247]; otherwise NULL
+ *            stands for c * 2^(exp - 127), exp in [27, 247] (infinite where that
+ *            is past bf16's range); otherwise NULL
  *   table    device int32 [n_req, max_pages]: request r's token at position p is
  *            in slot p % page of page table[r][p / page].  Entries past the
  *            context are not read.  Requests may share pages.  max_pages * page
@@ -448,7 +449,8 @@ lkv_status lkv_attn_prefill(const lkv_attn* attn, const int32_t* cu, int32_t n_s
  * nearest even, with e the least integer in [-100, 120] such that max |x| <=
  * 448 * 2^e; infinities and NaN do not count for e and become NaN.  (A power of
  * two costs a floating-point code no precision, and what is read back, 4
- * significant bits times 2^e, is exact in bf16.)
+ * significant bits times 2^e, is exact in bf16; with e = 120 codes past 240, whose
+ * values bf16 does not hold, are not used: magnitudes stop at 240 * 2^120.)
  *   k, v  [n_tok,h_kv,d] io_dtype.  Errors as for lkv_attn_prefill. */
 lkv_status lkv_kv_write(const lkv_attn* attn, const lkv_pages* pages, const int32_t* cu, int32_t n_req,
                         int64_t n_tok, const int32_t* pos, const void* k, int64_t k_stride,

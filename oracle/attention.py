@@ -43,14 +43,17 @@ def e4m3_codes(y):
 
 
 def e4m3_rows(x):
-    """Codes and exponent bytes of rows x [..., d]."""
+    """Codes and exponent bytes of rows x [..., d].  At the largest scale magnitudes stop at 240 * 2^120, the
+    largest that bf16 holds too."""
     x = np.asarray(x, np.float64)
     amax = np.max(np.abs(np.where(np.isfinite(x), x, 0.0)), axis=-1)
     e = np.full(amax.shape, -100)
     for i in np.ndindex(amax.shape):
         while e[i] < 120 and amax[i] > 448.0 * 2.0 ** e[i]:
             e[i] += 1
-    return e4m3_codes(x * 2.0 ** -e[..., None].astype(np.float64)), (e + 127).astype(np.uint8)
+    y = x * 2.0 ** -e[..., None].astype(np.float64)
+    y = np.where((e[..., None] == 120) & np.isfinite(y), np.clip(y, -240.0, 240.0), y)
+    return e4m3_codes(y), (e + 127).astype(np.uint8)
 
 
 def e4m3_values(codes, exps):

@@ -9,7 +9,8 @@
 //
 // e4m3 rows carry one power-of-two scale per (token, head).  A power of two costs a
 // floating-point code no precision, the scaling is exact, and so is the value read back: 4
-// significant bits times 2^e is a bf16 value.
+// significant bits times 2^e is a bf16 value.  At the largest scale, 2^120, codes stop at 240: the next,
+// 256 * 2^120, is past bf16's range, and the largest values would come back infinite.
 #include "attn_device.h"
 
 namespace lkv {
@@ -96,12 +97,13 @@ __device__ __forceinline__ u32x4 encode(const Raw<bf16>& r, int per_head, uint32
     amax = group_max(amax, per_head);
     byte = scale_byte(amax);
     const float inv = exp_scale((uint8_t)(254 - byte));  // 2^-e, exact
+    const float most = byte == 127 + 120 ? 240.f : 448.f;
     u32x4 out;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         float y[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) y[e] = __builtin_fabsf(x[4 * i + e]) < INFINITY ? x[4 * i + e] * inv : NAN;
+        for (int e = 0; e < 4; ++e) y[e] = __builtin_fabsf(x[4 * i + e]) < INFINITY ? __builtin_amdgcn_fmed3f(x[4 * i + e] * inv, -most, most) : NAN;
         int word = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
         word = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], word, true);
         out[i] = (uint32_t)word;

@@ -1,6 +1,9 @@
 """The full-attention calls at the limits of what they take: values that are infinite or NaN under weights
-that vanish, scores of -inf."""
+that vanish, scores of -inf, the largest bf16 values in an e4m3 cache."""
+import numpy as np
 import pytest
+
+from oracle import attention as A
 
 pytestmark = pytest.mark.gpu
 
@@ -9,7 +12,7 @@ if not torch.cuda.is_available():
     pytest.skip("no GPU", allow_module_level=True)
 
 from paper_2608_11231_amd import lkv  # noqa: E402
-from test_gpu_attn import BF, E4, F32, Cache, _attn_paged, _i32, _qkv  # noqa: E402
+from test_gpu_attn import BF, E4, F32, Cache, _attn_paged, _i32, _np, _qkv  # noqa: E402
 
 # name: h_q, h_kv, d, io, cache, context, new tokens; by `parts` the call's key range is split
 SPLIT = {
@@ -111,3 +114,26 @@ def test_a_token_without_keys_beside_values_not_finite():
         lkv.attn_paged(attn, C.pages, _i32([0, new]), new, q, o, ws)
         torch.cuda.synchronize()
         assert bool((o[:new - 3] == 0).all()) and bool(o[new - 3:].isnan().all())
+
+
+# ---------------------------------------------------------------- cache
+@pytest.mark.parametrize("hkv,d", [(1, 64), (4, 128), (8, 128)])
+def test_largest_values_in_e4m3(hkv, d):
+    """The largest finite bf16 values stay finite in an e4m3 cache."""
+    top = torch.finfo(BF).max
+    rows = [[top, -top, 1.0], [248 * 2.0 ** 120, -248 * 2.0 ** 120, 247 * 2.0 ** 120], [240 * 2.0 ** 120, 3e38, -3e38],
+            [top, float("inf"), float("nan")], [224 * 2.0 ** 120, 225 * 2.0 ** 120, 2.0 ** 127], [2.0 ** 127, top, 0.0]]
+    n = len(rows)
+    x = torch.zeros((n, hkv, d), dtype=BF)
+    x[:, :, :3] = torch.tensor(rows, dtype=torch.float64).to(BF)[:, None]
+    k, v = x.cuda(), x.flip(0).cuda()
+    attn = lkv.make_attn(hkv, hkv, d, page=16, cache_dtype=E4)
+    C = Cache(attn, [n])
+    lkv.kv_write(attn, C.pages, _i32([0, n]), n, k, v)
+    ko, vo = torch.empty_like(k), torch.empty_like(v)
+    lkv.kv_read(attn, C.pages, _i32([0, n]), n, ko, vo)
+    torch.cuda.synchronize()
+    for a, b in ((k, ko), (v, vo)):
+        want = A.e4m3_values(*A.e4m3_rows(_np(a)))
+        assert np.array_equal(_np(b), want, equal_nan=True)
+        assert bool((b.isfinite() == a.isfinite()).all())
