@@ -393,8 +393,11 @@ lkv_status lkv_state_rel_error(const float* S, const float* S_ref, int32_t n_sli
  * projection's output; o is dense.  cu: device int32 [n_req+1], cu[0] = 0, non-decreasing;
  * n_tok: host bound of cu[n_req].  Rows from cu[n_req] on are not touched, so
  * a padded batch (a captured graph's) may pass its capacity.  A call whose launch
- * would pass 2^24 workgroups is refused (LKV_E_SHAPE): 2^26 tokens of a write or
- * read, 2^28 rows (tokens * h_q) of attention for short requests and for fp32. */
+ * would have 2^24 workgroups or more is refused (LKV_E_SHAPE).  A write or read
+ * counts one per 4 tokens; attention (n_req + (n_tok * g - 1) / tile) * h_kv * parts,
+ * with g = h_q / h_kv, a tile of 128 rows (fp32: 32; paged calls of at most 16 rows
+ * n_tok * g per request on average: 16), and one part but in small paged calls.
+ * n_tok * h_q stays below 2^31, and so does n_req * h_kv + n_tok * h_q. */
 typedef struct {
     int32_t h_q;
     int32_t h_kv;
@@ -474,7 +477,8 @@ lkv_status lkv_kv_read(const lkv_attn* attn, const lkv_pages* pages, const int32
  *        same n_req, n_tok and max_pages; may be NULL if that is 0), 256-byte
  *        aligned, caller-owned; its contents on entry do not matter.  Calls that
  *        share a workspace race unless ordered by a stream.
- * Errors as for lkv_attn_prefill; LKV_E_SHAPE also for a workspace too small. */
+ * Errors as for lkv_attn_prefill; LKV_E_SHAPE also for a workspace too small.
+ * lkv_attn_paged_workspace refuses the sizes that the call refuses. */
 lkv_status lkv_attn_paged_workspace(const lkv_attn* attn, int32_t n_req, int64_t n_tok, int32_t max_pages,
                                     size_t* bytes);
 lkv_status lkv_attn_paged(const lkv_attn* attn, const lkv_pages* pages, const int32_t* cu, int32_t n_req,

@@ -681,6 +681,12 @@ AttnPlan attn_plan(const lkv_attn* A, int32_t n_req, int64_t n_tok, bool paged, 
     return p;
 }
 
+// Whether the launches of a paged call are taken
+bool plan_launches(const lkv_attn* A, const AttnPlan& p, int64_t n_tok) {
+    return launches((int64_t)std::max(p.tile_units, p.few_units) * A->h_kv * p.splits) &&
+           (p.splits == 1 || launches(n_tok * A->h_q));
+}
+
 struct AttnWs {
     size_t o, ml, total;
 };
@@ -1001,7 +1007,11 @@ lkv_status lkv_attn_paged_workspace(const lkv_attn* A, int32_t n_req, int64_t n_
     if (s == LKV_OK) s = check_counts(A, n_req, n_tok);
     if (s != LKV_OK) return s;
     if (max_pages < 0 || max_pages > MAX_CONTEXT / A->page) return LKV_E_SHAPE;
-    *bytes = n_req == 0 || n_tok == 0 ? 0 : attn_ws(A, n_tok, attn_plan(A, n_req, n_tok, true, max_pages).splits).total;
+    *bytes = 0;
+    if (n_req == 0 || n_tok == 0) return LKV_OK;
+    const AttnPlan plan = attn_plan(A, n_req, n_tok, true, max_pages);
+    if (!plan_launches(A, plan, n_tok)) return LKV_E_SHAPE;
+    *bytes = attn_ws(A, n_tok, plan.splits).total;
     return LKV_OK;
 }
 
@@ -1021,9 +1031,7 @@ lkv_status lkv_attn_paged(const lkv_attn* A, const lkv_pages* P, const int32_t* 
     a.pg = pages_args(A, P);
     const AttnPlan plan = attn_plan(A, n_req, n_tok, true, P->max_pages);
     a.splits = plan.splits;
-    if (!launches((int64_t)std::max(plan.tile_units, plan.few_units) * A->h_kv * a.splits) ||
-        (a.splits > 1 && !launches(n_tok * A->h_q)))
-        return LKV_E_SHAPE;
+    if (!plan_launches(A, plan, n_tok)) return LKV_E_SHAPE;
     const AttnWs w = attn_ws(A, n_tok, a.splits);
     if (w.total > 0) {
         if (!ws) return LKV_E_NULL;
