@@ -476,11 +476,16 @@ lkv_status lkv_kv_read(const lkv_attn* attn, const lkv_pages* pages, const int32
  *   ws   device workspace of at least lkv_attn_paged_workspace bytes (for the
  *        same n_req, n_tok and max_pages; may be NULL if that is 0), 256-byte
  *        aligned, caller-owned; its contents on entry do not matter.  Calls that
- *        share a workspace race unless ordered by a stream.
+ *        share a workspace race unless ordered by a stream.  A smaller call may need
+ *        more (its keys are split over more workgroups):
+ *        lkv_attn_paged_workspace_bound bytes are enough for every call of up to
+ *        n_tok tokens, in any requests, over tables up to max_pages wide (at most
+ *        128 parts of n_tok * h_q rows, and 393216 rows: 204 MB at d = 128).
  * Errors as for lkv_attn_prefill; LKV_E_SHAPE also for a workspace too small.
  * lkv_attn_paged_workspace refuses the sizes that the call refuses. */
 lkv_status lkv_attn_paged_workspace(const lkv_attn* attn, int32_t n_req, int64_t n_tok, int32_t max_pages,
                                     size_t* bytes);
+lkv_status lkv_attn_paged_workspace_bound(const lkv_attn* attn, int64_t n_tok, int32_t max_pages, size_t* bytes);
 lkv_status lkv_attn_paged(const lkv_attn* attn, const lkv_pages* pages, const int32_t* cu, int32_t n_req,
                           int64_t n_tok, const int32_t* pos, const void* q, int64_t q_stride, void* o,
                           void* ws, size_t ws_bytes, void* stream);

@@ -693,10 +693,23 @@ struct AttnWs {
 AttnWs attn_ws(const lkv_attn* A, int64_t n_tok, int splits) {
     AttnWs w = {};
     if (splits <= 1) return w;
-    const size_t rows = (size_t)splits * n_tok * A->h_q;
+    const size_t rows = (size_t)splits * n_tok * A->h_q;  // of all parts
     w.ml = (rows * A->d * 4 + 255) & ~size_t(255);
     w.total = w.ml + rows * 8;
     return w;
+}
+
+// Most workspace of any call of up to n_tok tokens over up to `context` keys, by attn_plan's rules: at
+// most MAX_PARTS parts, of 256 keys at least; and with w workgroups of T rows fewer than 2048 / w + 1 parts
+// (few rows: with w up to 256, 512 / w), so rows * parts < T * (2048 + w): tiles have T = 128 (fp32: 32)
+// and w < 1024, few rows T = 32 at most and w < 2048.
+size_t attn_ws_bound(const lkv_attn* A, int64_t n_tok, int64_t context) {
+    const int64_t parts = std::min((context + 255) / 256, MAX_PARTS);
+    if (parts <= 1) return 0;
+    const int64_t most = A->io_dtype == LKV_F32 ? ATTN_ROWS_F32 * (2048 + 1024)
+                                                : std::max(ATTN_ROWS * (2048 + 1024), FEW_ROWS * (2048 + 2048));
+    const size_t rows = (size_t)std::min(parts * n_tok * A->h_q, most);
+    return ((rows * A->d * 4 + 255) & ~size_t(255)) + rows * 8;
 }
 
 lkv_status kv_move(const lkv_attn* A, const lkv_pages* P, const int32_t* cu, int32_t n_req, int64_t n_tok,
@@ -1012,6 +1025,16 @@ lkv_status lkv_attn_paged_workspace(const lkv_attn* A, int32_t n_req, int64_t n_
     const AttnPlan plan = attn_plan(A, n_req, n_tok, true, max_pages);
     if (!plan_launches(A, plan, n_tok)) return LKV_E_SHAPE;
     *bytes = attn_ws(A, n_tok, plan.splits).total;
+    return LKV_OK;
+}
+
+lkv_status lkv_attn_paged_workspace_bound(const lkv_attn* A, int64_t n_tok, int32_t max_pages, size_t* bytes) {
+    if (!bytes) return LKV_E_NULL;
+    lkv_status s = check_attn(A);
+    if (s == LKV_OK) s = check_counts(A, 0, n_tok);
+    if (s != LKV_OK) return s;
+    if (max_pages < 0 || max_pages > MAX_CONTEXT / A->page) return LKV_E_SHAPE;
+    *bytes = attn_ws_bound(A, n_tok, (int64_t)max_pages * A->page);
     return LKV_OK;
 }
 

@@ -64,7 +64,7 @@ EXPORTS = ("lkv_abi_version", "lkv_status_string", "lkv_last_hip_error", "lkv_bl
            "lkv_init_compose_bf16", "lkv_round_bf16", "lkv_stage_rows", "lkv_state_rel_error",
            "lkv_chunk_scan_from_pool", "lkv_set_wait_limit", "lkv_chunk_scan_sp_workspace",
            "lkv_chunk_scan_sp", "lkv_chunk_scan_sp_noalloc", "lkv_attn_prefill", "lkv_kv_write", "lkv_kv_read",
-           "lkv_attn_paged_workspace", "lkv_attn_paged")
+           "lkv_attn_paged_workspace", "lkv_attn_paged_workspace_bound", "lkv_attn_paged")
 
 
 def load() -> ctypes.CDLL:
@@ -108,12 +108,13 @@ def load() -> ctypes.CDLL:
             lib.lkv_kv_write.argtypes = [AP, PP, vp, i32, i64, vp, vp, i64, vp, i64, vp]
             lib.lkv_kv_read.argtypes = [AP, PP, vp, i32, i64, vp, vp, i64, vp, i64, vp]
             lib.lkv_attn_paged_workspace.argtypes = [AP, i32, i64, i32, ctypes.POINTER(ctypes.c_size_t)]
+            lib.lkv_attn_paged_workspace_bound.argtypes = [AP, i64, i32, ctypes.POINTER(ctypes.c_size_t)]
             lib.lkv_attn_paged.argtypes = [AP, PP, vp, i32, i64, vp, vp, i64, vp, vp, ctypes.c_size_t, vp]
             for f in ("lkv_block_summary", "lkv_init_single", "lkv_init_compose", "lkv_gdn_chunk_scan",
                       "lkv_ssd_chunk_scan", "lkv_gdn_decode", "lkv_ssd_decode", "lkv_gather_selected",
                       "lkv_init_single_bf16", "lkv_init_compose_bf16", "lkv_round_bf16", "lkv_stage_rows",
                       "lkv_state_rel_error", "lkv_chunk_scan_from_pool", "lkv_attn_prefill", "lkv_kv_write", "lkv_kv_read",
-                      "lkv_attn_paged_workspace", "lkv_attn_paged"):
+                      "lkv_attn_paged_workspace", "lkv_attn_paged_workspace_bound", "lkv_attn_paged"):
                 getattr(lib, f).restype = ctypes.c_int
             _lib = lib
     return _lib
@@ -455,10 +456,18 @@ def kv_read(attn: Attn, pages: Pages, cu: torch.Tensor, n_tok: int, k: torch.Ten
 
 
 def attn_paged_workspace(attn: Attn, n_req: int, n_tok: int, max_pages: int) -> int:
-    """Workspace bytes of attn_paged."""
+    """Workspace bytes of attn_paged.  A smaller call may need more: see attn_paged_workspace_bound."""
     n = ctypes.c_size_t(0)
     _check(load().lkv_attn_paged_workspace(attn, int(n_req), int(n_tok), int(max_pages), ctypes.byref(n)),
            "lkv_attn_paged_workspace")
+    return int(n.value)
+
+
+def attn_paged_workspace_bound(attn: Attn, n_tok: int, max_pages: int) -> int:
+    """Workspace bytes that are enough for every attn_paged of up to n_tok tokens over tables up to max_pages wide."""
+    n = ctypes.c_size_t(0)
+    _check(load().lkv_attn_paged_workspace_bound(attn, int(n_tok), int(max_pages), ctypes.byref(n)),
+           "lkv_attn_paged_workspace_bound")
     return int(n.value)
 
 

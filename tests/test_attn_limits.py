@@ -1,5 +1,6 @@
 """The full-attention layers' format and sizes at their limits, on the CPU."""
 import ctypes
+import random
 
 import numpy as np
 import pytest
@@ -36,3 +37,33 @@ def test_launches_at_their_limit(per, heads, io):
         r = (lo + hi) // 2
         lo, hi = (r, hi) if (r + (r * per - 1) // rows) * heads < 1 << 24 else (lo, r)
     assert status(lo) == 0 and status(hi) == 2 and hi * per * heads < 1 << 31
+
+
+BOUND_LAYERS = [(8, 8, 128, 1, 1), (32, 8, 128, 1, 1), (32, 8, 128, 1, 2), (16, 2, 256, 1, 1), (16, 2, 256, 1, 2), (6, 1, 64, 1, 1),
+                (64, 1, 64, 1, 2), (3, 3, 64, 0, 0), (8, 2, 128, 0, 0), (1, 1, 64, 1, 1)]
+
+
+@pytest.mark.parametrize("hq,hkv,d,io,cache", BOUND_LAYERS)
+def test_a_workspace_for_every_smaller_call(hq, hkv, d, io, cache):
+    """The bound over a batch holds for the batch and for every smaller one: all of few requests and tokens,
+    and numbers of either spread over their ranges."""
+    a = lkv.Attn(h_q=hq, h_kv=hkv, d=d, page=16, io_dtype=io, cache_dtype=cache, scale=0.1)
+    rng = random.Random(hq * d + cache)
+    spread = lambda hi: int(round(hi ** rng.random()))  # noqa: E731
+    calls = [(r, t, p) for r in range(1, 20) for t in range(1, 40) for p in (17, 4096)]
+    calls += [(spread(5000), spread(200000), spread(1 << 17)) for _ in range(20000)]
+    need = sorted((t, p, lkv.attn_paged_workspace(a, r, t, p)) for r, t, p in calls)
+    for n_tok, width in [(1, 4096), (39, 17), (39, 1 << 17), (300, 1 << 10), (5000, 1 << 17), (200000, 1 << 12), (200000, 1 << 17)]:
+        bound = lkv.attn_paged_workspace_bound(a, n_tok, width)
+        most = max(n for t, p, n in need if t <= n_tok and p <= width)
+        assert most <= bound <= 393216 * (4 * d + 8) and (bound == 0) == (most == 0)
+    assert lkv.attn_paged_workspace_bound(a, 0, 1 << 17) == lkv.attn_paged_workspace_bound(a, 100, 16) == 0
+
+
+def test_bound_arguments():
+    f, n = lkv.load().lkv_attn_paged_workspace_bound, ctypes.c_size_t(0)
+    a = lkv.Attn(h_q=8, h_kv=2, d=128, page=64, io_dtype=1, cache_dtype=1, scale=0.1)
+    bad = lkv.Attn(h_q=8, h_kv=2, d=96, page=64, io_dtype=1, cache_dtype=1, scale=0.1)
+    assert f(a, 4, 2, None) == f(None, 4, 2, ctypes.byref(n)) == 1 and f(bad, 4, 2, ctypes.byref(n)) == 5
+    assert f(a, -1, 2, ctypes.byref(n)) == f(a, 1 << 31, 2, ctypes.byref(n)) == f(a, 4, -1, ctypes.byref(n)) == 2
+    assert f(a, 4, 1 << 26, ctypes.byref(n)) == 2

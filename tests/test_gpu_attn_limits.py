@@ -1,5 +1,5 @@
 """The full-attention calls at the limits of what they take: values that are infinite or NaN under weights
-that vanish, scores of -inf, the largest bf16 values in an e4m3 cache."""
+that vanish, scores of -inf, the largest bf16 values in an e4m3 cache, one workspace for many batches."""
 import numpy as np
 import pytest
 
@@ -137,3 +137,23 @@ def test_largest_values_in_e4m3(hkv, d):
         want = A.e4m3_values(*A.e4m3_rows(_np(a)))
         assert np.array_equal(_np(b), want, equal_nan=True)
         assert bool((b.isfinite() == a.isfinite()).all())
+
+
+# ---------------------------------------------------------------- workspace
+def test_one_workspace_for_every_batch():
+    """A workspace by the bound of the largest batch serves the smaller ones, which need more of it."""
+    attn = lkv.make_attn(8, 2, 128, page=16)
+    rng = np.random.default_rng(5)
+    C = Cache(attn, [int(c) for c in rng.integers(1, 4000, 600)])
+    C.fill()
+    width = C.table.shape[1]
+    ws = torch.empty(lkv.attn_paged_workspace_bound(attn, 600, width), dtype=torch.uint8, device="cuda")
+    assert lkv.attn_paged_workspace(attn, 600, 600, width) < lkv.attn_paged_workspace(attn, 7, 420, width) <= ws.numel()
+    for n_req, m in ((600, 1), (40, 5), (7, 60), (1, 600), (1, 1)):
+        q = _qkv(n_req * m, 8, 1, 128, BF, n_req)[0]
+        cu = np.arange(n_req + 1) * m
+        want = _attn_paged(attn, C, cu, q)
+        o, ws[:] = torch.full_like(want, 7.0), 255
+        lkv.attn_paged(attn, C.pages, _i32(cu), n_req * m, q, o, ws)
+        torch.cuda.synchronize()
+        assert torch.equal(o, want)
