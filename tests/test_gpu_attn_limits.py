@@ -1,5 +1,6 @@
 """The full-attention calls at the limits of what they take: values that are infinite or NaN under weights
-that vanish, scores of -inf, the largest bf16 values in an e4m3 cache, one workspace for many batches."""
+that vanish, scores of -inf, the largest bf16 values in an e4m3 cache, one workspace for many batches, fp32
+tokens in their rarer forms."""
 import numpy as np
 import pytest
 
@@ -12,7 +13,7 @@ if not torch.cuda.is_available():
     pytest.skip("no GPU", allow_module_level=True)
 
 from paper_2608_11231_amd import lkv  # noqa: E402
-from test_gpu_attn import BF, E4, F32, Cache, _attn_paged, _i32, _np, _qkv  # noqa: E402
+from test_gpu_attn import BF, E4, F32, Cache, _attn_paged, _check_paged, _cum, _i32, _np, _qkv  # noqa: E402
 
 # name: h_q, h_kv, d, io, cache, context, new tokens; by `parts` the call's key range is split
 SPLIT = {
@@ -157,3 +158,43 @@ def test_one_workspace_for_every_batch():
         lkv.attn_paged(attn, C.pages, _i32(cu), n_req * m, q, o, ws)
         torch.cuda.synchronize()
         assert torch.equal(o, want)
+
+
+@pytest.mark.parametrize("hkv,d,page", [(3, 128, 32), (9, 64, 16), (5, 128, 1024)])
+def test_write_and_read_of_many_fp32_heads(hkv, d, page):
+    """Tokens that a whole wave moves, in more than one round of its lanes among them."""
+    attn = lkv.make_attn(hkv, hkv, d, page=page, io_dtype=F32)
+    ctx, new = [300, 0, 90, 1], [130, 0, 90, 1]
+    C = Cache(attn, ctx)
+    rng = np.random.default_rng(3)
+    pos = np.concatenate([rng.choice(c, m, replace=False) for c, m in zip(ctx, new)]).astype(np.int32)
+    pos[[4, 140]] = [300, -1]
+    n = sum(new)
+    _, k, v = _qkv(n + 2, 1, hkv, d, F32, 4)
+    ko, vo = (torch.full((n + 2, hkv, d), 7.0, device="cuda") for _ in range(2))
+    at = _i32(np.append(pos, [0, 0]))
+    lkv.kv_write(attn, C.pages, _i32(_cum(new)), n + 2, k, v, at)
+    lkv.kv_read(attn, C.pages, _i32(_cum(new)), n + 2, ko, vo, at)
+    torch.cuda.synchronize()
+    for x, o in ((k, ko), (v, vo)):
+        want = _np(x)
+        want[[4, 140]] = np.nan
+        want[n:] = 7.0
+        assert np.array_equal(_np(o), want, equal_nan=True)
+    assert int((~C.k.isnan()).all(-1).all(1).sum()) == n - 2
+
+
+# ---------------------------------------------------------------- attention
+@pytest.mark.parametrize("hq,hkv,d", [(4, 2, 64), (3, 3, 128)])
+@pytest.mark.parametrize("ctx,new", [([9000], [1]), ([12000, 5, 3000], [3, 7, 1])], ids=str)
+def test_fp32_over_many_parts(hq, hkv, d, ctx, new):
+    """Few fp32 rows over more than eight parts of the key range, rows that see nothing among them."""
+    attn = lkv.make_attn(hq, hkv, d, page=64, io_dtype=F32)
+    C = Cache(attn, ctx)
+    size = lkv.attn_paged_workspace(attn, len(ctx), sum(new) + 1, C.table.shape[1])
+    assert size > 8 * (sum(new) + 1) * hq * (4 * d + 8) + 256 and (sum(new) + 1) * hq < 1024
+    C.fill()
+    q = _qkv(sum(new) + 1, hq, 1, d, F32, 6)[0]
+    o = _attn_paged(attn, C, _cum(new), q)
+    _check_paged(attn, C, new, q, o)
+    assert bool((o[sum(new):] == 7.0).all())
