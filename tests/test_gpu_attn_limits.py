@@ -1,6 +1,6 @@
 """The full-attention calls at the limits of what they take: values that are infinite or NaN under weights
 that vanish, scores of -inf, the largest bf16 values in an e4m3 cache, one workspace for many batches, fp32
-tokens in their rarer forms."""
+tokens in their rarer forms, probabilities that are all rounded one way."""
 import numpy as np
 import pytest
 
@@ -198,3 +198,45 @@ def test_fp32_over_many_parts(hq, hkv, d, ctx, new):
     o = _attn_paged(attn, C, _cum(new), q)
     _check_paged(attn, C, new, q, o)
     assert bool((o[sum(new):] == 7.0).all())
+
+
+def _one_way_keys(n_one, n_down):
+    """Keys of scores s (q = 1, 1, 0 ..): exp(s) = 1, then just below 1 + 2^-8, which bf16 rounds down to 1,
+    and a last one just above, rounded up to 1 + 2^-7."""
+    tie = np.log1p(2.0 ** -8)
+    s = np.concatenate([np.zeros(n_one), np.full(n_down, tie - 2e-6), [tie + 2e-6]])
+    hi = torch.from_numpy(s).to(BF)
+    lo = (torch.from_numpy(s) - hi.double()).to(BF)
+    k = torch.zeros((len(s), 1, 64), dtype=BF)
+    k[:, 0, 0], k[:, 0, 1] = hi, lo
+    return k
+
+
+@pytest.mark.parametrize("call,n_req,m", [("prefill", 1, 6257), ("one_token", 2048, 1), ("chunk", 350, 130)])
+def test_probabilities_rounded_one_way(call, n_req, m):
+    """Tolerance: a probability is off by 2^-8 of itself at most, and so is their sum (which is of the rounded
+    ones, so that weights add up to 1): 2 * 2^-8 of A = sum_j p_j |v_j| for the weights, 2^-8 for the
+    output, and 2^-10 for products of these and all that is fp32.  Here the roundings add up: nearly all
+    probabilities are rounded down, and that of the one key with a value, up.  The requests share their
+    pages and are as many as leave the key range whole."""
+    k = _one_way_keys(256, 6000).cuda()
+    n = k.shape[0]
+    v = torch.zeros((n, 1, 64), dtype=BF, device="cuda")
+    v[-1, 0] = torch.linspace(1, 2, 65)[:64].to(BF).cuda()
+    q = torch.zeros((n_req * m, 2, 64), dtype=BF, device="cuda")
+    q[:, :, :2] = 1.0
+    attn = lkv.make_attn(2, 1, 64, scale=1.0, page=64)
+    o = torch.full_like(q, 7.0)
+    if call == "prefill":
+        lkv.attn_prefill(attn, _i32([0, n]), n, q, k, v, o)
+    else:
+        C = Cache(attn, [n])
+        lkv.kv_write(attn, C.pages, _i32([0, n]), n, k, v)
+        pages = lkv.make_pages(attn, C.k, C.v, _i32(np.repeat(C.table, n_req, 0)), _i32([n] * n_req))
+        assert lkv.attn_paged_workspace(attn, n_req, n_req * m, C.table.shape[1]) == 0
+        lkv.attn_paged(attn, pages, _i32(np.arange(n_req + 1) * m), n_req * m, q, o, None)
+    torch.cuda.synchronize()
+    ref, mag, _ = A.attention(_np(q[-1:]), _np(k), _np(v), [n - 1], 1.0)
+    last = o.view(n_req, m, 2, 64)[:, -1]
+    assert bool((last == last[:1]).all()) and bool((o.view(n_req, m, 2, 64)[:, :-1] == 0).all())
+    assert np.max(np.abs(_np(last[:1]) - ref) / mag) <= 3 * 2.0 ** -8 + 2.0 ** -10
