@@ -378,7 +378,7 @@ lkv_status lkv_state_rel_error(const float* S, const float* S_ref, int32_t n_sli
  *                but checked)
  *   io_dtype     dtype of q, k, v and o          LKV_F32 (d <= 128) | LKV_BF16
  *   cache_dtype  dtype of the pages              io_dtype, or LKV_E4M3 with LKV_BF16
- *   scale        softmax scale, finite and > 0
+ *   scale        softmax scale, > 0 and at most 2^127
  *
  * A token at position p attends to its request's keys 0..p: with s_j = scale
  * q.k_j, o = sum_j exp(s_j) v_j / sum_j exp(s_j).  Scores, statistics and sums

@@ -530,7 +530,7 @@ constexpr int32_t MAX_CONTEXT = 1 << 30;
 lkv_status check_attn(const lkv_attn* A) {
     if (!A) return LKV_E_NULL;
     if (A->h_q < 1 || A->h_kv < 1 || A->h_q % A->h_kv != 0 || A->d < 1 || A->page < 1) return LKV_E_SHAPE;
-    if (!(A->scale > 0.f) || !isfinite(A->scale)) return LKV_E_SHAPE;
+    if (!(A->scale > 0.f) || A->scale > 0x1p127f) return LKV_E_SHAPE;  // times log2(e) it is finite
     if (A->io_dtype != LKV_F32 && A->io_dtype != LKV_BF16) return LKV_E_DTYPE;
     if (A->cache_dtype != A->io_dtype && !(A->cache_dtype == LKV_E4M3 && A->io_dtype == LKV_BF16)) return LKV_E_DTYPE;
     if (A->d != 64 && A->d != 128 && !(A->d == 256 && A->io_dtype == LKV_BF16)) return LKV_E_UNSUPPORTED;

@@ -67,3 +67,11 @@ def test_bound_arguments():
     assert f(a, 4, 2, None) == f(None, 4, 2, ctypes.byref(n)) == 1 and f(bad, 4, 2, ctypes.byref(n)) == 5
     assert f(a, -1, 2, ctypes.byref(n)) == f(a, 1 << 31, 2, ctypes.byref(n)) == f(a, 4, -1, ctypes.byref(n)) == 2
     assert f(a, 4, 1 << 26, ctypes.byref(n)) == 2
+
+
+def test_largest_scale():
+    """A scale whose product with log2(e) is past fp32's range would make NaN of scores that are 0."""
+    n = ctypes.c_size_t(0)
+    for scale, status in ((2.0 ** 127, 0), (3e38, 2), (1e-38, 0), (float("inf"), 2)):
+        a = lkv.Attn(h_q=8, h_kv=2, d=128, page=64, io_dtype=1, cache_dtype=1, scale=scale)
+        assert lkv.load().lkv_attn_paged_workspace(a, 1, 4, 2, ctypes.byref(n)) == status
