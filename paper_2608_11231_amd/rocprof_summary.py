@@ -6,6 +6,8 @@
 
     python -m paper_2608_11231_amd.rocprof_summary counters <out.txt> <counter_collection.csv>... -- <command...>
 
+Take them with --mangled-kernels: rocprofv3's own demangler garbles names with bf16 template arguments.
+
 ``traffic`` calibrates FETCH_SIZE / WRITE_SIZE on the plain device copy that
 ``bench.py --copy-probe`` launches (copy_bytes read and written), scales every
 kernel's per-dispatch counters by those factors and records the hash of the
@@ -19,6 +21,7 @@ import csv
 import glob
 import hashlib
 import os
+import re
 import sys
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -33,7 +36,31 @@ def kernel_source_hash() -> str:
     return h.hexdigest()[:16]
 
 
+def demangle(name: str) -> str:
+    """lkv::kernel<arguments> of a mangled kernel of this library whose template arguments are integers, truth
+    values and bf16 or float; any other name as it is."""
+    m = re.match(r"_ZN3lkv(\d+)", name)
+    if not m:
+        return name
+    end = m.end() + int(m[1])
+    base, rest = "lkv::" + name[m.end():end], name[end:]
+    if not rest.startswith("I"):
+        return base
+    args, rest = [], rest[1:]
+    while not rest.startswith("E"):
+        a = re.match(r"L([ib])(n?)(\d+)E|(DF16b)|(f)", rest)
+        if not a:
+            return name
+        rest = rest[a.end():]
+        if a[1]:
+            args.append(("false", "true")[int(a[3])] if a[1] == "b" else a[2].replace("n", "-") + a[3])
+        else:
+            args.append("bf16" if a[4] else "float")
+    return f"{base}<{','.join(args)}>"
+
+
 def short_name(name: str) -> str:
+    name = demangle(name)
     name = name.replace("void ", "")
     name = name.split("(")[0] if "(" in name else name
     return name.replace(" ", "")
@@ -42,12 +69,14 @@ def short_name(name: str) -> str:
 def trace(trace_csv: str, out: str, command: str) -> None:
     """Per (kernel, grid) dispatch durations from a --kernel-trace CSV: count,
     median, mean, min, max.  The median separates a kernel's steady-state
-    launches from a one-off launch of the same symbol and grid."""
-    groups = collections.defaultdict(list)
+    launches from a one-off launch of the same symbol and grid.  Kernels that are
+    not this library's (copies, the preparation of inputs) share one line."""
+    groups, others = collections.defaultdict(list), []
     for r in csv.DictReader(open(trace_csv)):
         grid = int(r["Grid_Size_X"]) * int(r["Grid_Size_Y"]) * int(r["Grid_Size_Z"])
         dur = (int(r["End_Timestamp"]) - int(r["Start_Timestamp"])) / 1e3
-        groups[(short_name(r["Kernel_Name"]), grid)].append(dur)
+        name = short_name(r["Kernel_Name"])
+        (groups[(name, grid)] if name.startswith("lkv::") else others).append(dur)
     lines = ["# rocprofv3 kernel trace, per-dispatch durations (us)", f"command: {command}",
              f"kernel_source_hash: {kernel_source_hash()}", "",
              f"{'kernel':60s} {'grid':>9s} {'calls':>6s} {'median_us':>10s} {'mean_us':>10s} {'min_us':>10s} "
@@ -57,6 +86,7 @@ def trace(trace_csv: str, out: str, command: str) -> None:
         med = d[len(d) // 2]
         lines.append(f"{name[:60]:60s} {grid:9d} {len(d):6d} {med:10.2f} {sum(d) / len(d):10.2f} {d[0]:10.2f} "
                      f"{d[-1]:10.2f}")
+    lines += ["", f"other kernels (copies, preparation of inputs): {len(others)} dispatches, {sum(others):.0f} us"]
     open(out, "w").write("\n".join(lines) + "\n")
 
 
@@ -123,7 +153,9 @@ def counters(out: str, paths, command: str) -> None:
     """Per (kernel, grid): the median over its dispatches of every SQ/GRBM counter
     in the given --pmc runs, and derived shares of the dispatch's cycles.
     GRBM_GUI_ACTIVE is summed over the 8 XCDs, so the dispatch's cycles are
-    GRBM_GUI_ACTIVE / 8 (``clock_GHz`` checks that against the dispatch time).
+    GRBM_GUI_ACTIVE / 8 (``clock_GHz`` checks that against the dispatch time).  They
+    span some 15000 cycles more than the dispatch, so the shares of short dispatches
+    are low, and below 100 us no clock is derived.
     A wave64 VALU instruction holds its SIMD for 4 cycles, and
     SQ_ACTIVE_INST_VALU counts about one unit per instruction, i.e. quad-cycles:
       mfma_busy    = SQ_VALU_MFMA_BUSY_CYCLES / (cycles * 1024 SIMDs)
@@ -150,7 +182,8 @@ def counters(out: str, paths, command: str) -> None:
              "derived: cycles = GRBM_GUI_ACTIVE / 8 XCDs; mfma_busy = SQ_VALU_MFMA_BUSY_CYCLES / "
              "(cycles * 1024); valu_busy = 4 * SQ_ACTIVE_INST_VALU / (cycles * 1024); lds_busy = "
              "SQ_LDS_IDX_ACTIVE / (cycles * 256); lds_conflict = SQ_LDS_BANK_CONFLICT / SQ_LDS_IDX_ACTIVE; "
-             "per_wave = SQ_INSTS_* / SQ_WAVES", ""]
+             "per_wave = SQ_INSTS_* / SQ_WAVES; cycles span some 15000 more than the dispatch, so shares of short "
+             "dispatches are low and their clock is left out", ""]
     for (name, grid), cs in sorted(groups.items()):
         if not name.startswith("lkv::"):
             continue
@@ -164,7 +197,7 @@ def counters(out: str, paths, command: str) -> None:
         gui = m.get("GRBM_GUI_ACTIVE")
         if gui:
             cyc = gui / N_XCD
-            if m.get("duration_us"):
+            if m.get("duration_us", 0) >= 100:
                 der.append(f"clock_GHz {cyc / (m['duration_us'] * 1e3):.2f}")
             if m.get("SQ_VALU_MFMA_BUSY_CYCLES") is not None:
                 der.append(f"mfma_busy {m['SQ_VALU_MFMA_BUSY_CYCLES'] / (cyc * N_SIMD):.3f}")
