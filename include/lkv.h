@@ -482,7 +482,9 @@ lkv_status lkv_kv_read(const lkv_attn* attn, const lkv_pages* pages, const int32
  *        n_tok tokens, in any requests, over tables up to max_pages wide (at most
  *        128 parts of n_tok * h_q rows, and 393216 rows: 204 MB at d = 128).
  * Errors as for lkv_attn_prefill; LKV_E_SHAPE also for a workspace too small.
- * lkv_attn_paged_workspace refuses the sizes that the call refuses. */
+ * lkv_attn_paged_workspace refuses the sizes that the call refuses.  Keys are split
+ * by max_pages, so short contexts are read fastest through a table no wider than
+ * the longest of them. */
 lkv_status lkv_attn_paged_workspace(const lkv_attn* attn, int32_t n_req, int64_t n_tok, int32_t max_pages,
                                     size_t* bytes);
 lkv_status lkv_attn_paged_workspace_bound(const lkv_attn* attn, int64_t n_tok, int32_t max_pages, size_t* bytes);

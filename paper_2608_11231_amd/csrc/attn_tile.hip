@@ -12,8 +12,9 @@
 // for the product (2^-8 of each at most, as the outputs are).
 //
 // Power bounds the large calls (two workgroups per CU: the clock falls to 2.0 GHz with the matrix
-// cores half busy): a 32K prompt of 32/8 heads of 128 takes 8.1 to 8.5 ms, 1.06 PFLOP/s; an 8K
-// prompt of 16/2 heads of 256 0.51 to 0.58 ms, 1.0 PFLOP/s.  Measured beside it and not better: the
+// cores half busy): a 32K prompt of 32/8 heads of 128 takes 8.3 ms on new inputs, 1.06 PFLOP/s (8.2 on
+// inputs at rest in the caches; up to 9.0 on other cards and under the profiler), an 8K prompt of
+// 16/2 heads of 256 0.57 ms, 0.97 PFLOP/s (0.52; 0.60).  Measured beside it and not better: the
 // next tile's scores formed in between softmax and product (8.3 ms), eight waves that share a tile
 // (8.4), three waves per SIMD on tiles of 32 keys (8.2; 32 ragged blocks 490 against 460 us), keys
 // staged through registers (8.0 with eight waves, but paged keys 6.2 against 4.7 ms), 64 rows per
@@ -476,9 +477,13 @@ static hipError_t launch_d(int kind, bool paged, const AttnArgs& a, hipStream_t 
     const int64_t wgs = (int64_t)a.n_units * a.h_kv * (paged ? a.splits : 1);
     const dim3 grid((unsigned)wgs), block(64 * NW);
     // Two groups where the launch does not fill the GPU with workgroups, two a CU, and the chains are
-    // long (a prompt of 4096, 8 heads of 128: 88 -> 68 us; 2048, 16/2 heads of 256: 116 -> 76; filled, or
+    // long (a prompt of 4096, 8 heads of 128: 87 -> 66 us; 2048, 16/2 heads of 256: 117 -> 74; filled, or
     // short, the join and the rounds in step cost more: 16384, 8 heads of 128, 553 -> 607; four of
-    // 300, 32/8 heads of 128, 15 -> 21).  Paged calls split their keys over workgroups instead.
+    // 300, 32/8 heads of 128, 15 -> 21).  The limit is a line under the measured borders, alike for the
+    // three d: 512 tokens gain at 256 workgroups (d = 128: 17.8 -> 16.7 us) and lose at 320 (20.8 -> 22.2),
+    // 768 even out at 384 (26.0, 25.5), 1024 gain at 384 (32.6 -> 30.4) and not at 512 (33.2, 33.7), 2048
+    // and more gain up to 512 (58.6 -> 51.1) and lose at 640 (62.3 -> 72.1).  Paged calls split their
+    // keys over workgroups instead.
     const int64_t mean = a.n_tok / a.n_req;
     const bool two = !paged && mean >= 512 && wgs <= std::min<int64_t>(512, mean * 3 / 8);
     if (two) hipLaunchKernelGGL((attn_tile_kernel<D, KV_BF16, false, 2>), grid, dim3(128 * NW), 0, st, a);

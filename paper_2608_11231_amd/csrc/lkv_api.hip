@@ -616,6 +616,10 @@ AttnArgs attn_args(const lkv_attn* A, const int32_t* cu, int32_t n_req, int64_t 
 // few rows costs more than that overlap gains, and requests of up to 32 rows get their own kernel
 // (the same, heads of 64: 214 against 283 us; a chunk of 2048 beside 30 tokens of 8K, heads of 128: 413
 // against 477; with heads of 256, where its 32 rows fill a CU, 338 against 280: not there).
+// The mean does not show a chunk among single tokens: just under its border the few-row kernel reads the
+// chunk's context once per 16 rows.  32/8 heads of 128 over 1K, here against the tiles alone: 256 single
+// tokens and a chunk of 512 in bf16 224 us against 218, in e4m3 139 against 151; 1000 and 2048 930
+// against 785, 579 against 497; 256 without a chunk 184 against 195, 104 against 114.
 struct AttnPlan {
     int few_rows;    // row tile of attn_few_kernel, 0: not launched
     int few_units;   // (request, row tile) pairs at most
@@ -646,7 +650,10 @@ AttnPlan attn_plan(const lkv_attn* A, int32_t n_req, int64_t n_tok, bool paged, 
             p.few_units = n_req;  // one tile each
         }
     }
-    // Parts of the key range, none below 256 keys of the longest context.  Few rows: where the
+    // Parts of the key range, none below 256 keys of the longest context that the table has room for: a
+    // table wider than its contexts makes more and shorter parts than they want (64 single tokens over
+    // 1K, 8 heads of 128, tables of 1K and of 32K: bf16 43 and 51 us, e4m3 24 and 36; contexts of 8K
+    // the same with both).  Few rows: where the
     // requests leave CUs idle, one round of the workgroups that the GPU holds (four contexts of 8K,
     // 8 heads: 28.4 us with 16 parts, 30.1 with 32); else more and smaller workgroups, so that the
     // longest contexts do not end alone (48 of 1K-8K, 8 heads of 128: 213 us whole, 173 in 6; 128: 467
