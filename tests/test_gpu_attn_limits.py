@@ -15,7 +15,7 @@ if not torch.cuda.is_available():
 from paper_2608_11231_amd import lkv  # noqa: E402
 from test_gpu_attn import BF, E4, F32, Cache, _attn_paged, _check_paged, _cum, _i32, _np, _qkv  # noqa: E402
 
-# name: h_q, h_kv, d, io, cache, context, new tokens; by `parts` the call's key range is split
+# name: h_q, h_kv, d, io, cache, context, new tokens; SPLIT: calls whose key range is split
 SPLIT = {
     "one_token_8_parts": (8, 2, 128, BF, BF, 2000, 1),
     "one_token_36_parts": (8, 2, 128, BF, BF, 9000, 1),
